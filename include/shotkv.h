@@ -107,6 +107,42 @@ SHOTKV_API int shotkv_validate(const shotkv_dims* dims, const shotkv_policy* pol
  * buffer of this size serves all).  0 on invalid dims.  */
 SHOTKV_API size_t shotkv_workspace_bytes(const shotkv_dims* dims);
 
+/* ---- before the compression: norm, rotation, layout ------------------------------------------ */
+
+/* What shotkv_norm_rope does with a layer's projected rows. */
+typedef struct {
+    int32_t layer;             /* l of the tensors written: 0 .. L-1                                */
+    int32_t first, rows;       /* the rows are prompt positions first .. first+rows-1 of N          */
+    int32_t rot;               /* elements of a head that are rotated: a multiple of 16, 0 .. d     */
+    int32_t interleaved;       /* pairs (a, b): 0 = elements (i, i + rot/2), 1 = (2i, 2i + 1)       */
+    int32_t table_rows;        /* rows of cos_sin                                                   */
+    float   eps;               /* of the norms                                                      */
+    int64_t q_row, k_row, v_row;          /* elements from one row's heads to the next row's ...    */
+    int64_t q_prompt, k_prompt, v_prompt; /* ... and from one prompt's to the next: multiples of 8  */
+} shotkv_rope;
+
+/* Queries and keys normed per head and rotated by position, values as they are, each written where the other calls
+ * read it: what stands between a layer's projection and the prefill calls, or (with N = W = rows = 1) the decode
+ * step.  Per head of d elements, in 32 bits, rounded to bf16 once:
+ *   y = x / sqrt(mean(x^2) + eps) * weight          where a weight is given, else y = x
+ *   (a, b) -> (a cos - b sin, b cos + a sin)        for the pairs of the first rot elements
+ *   q, k, v    device bf16, heads of d contiguous elements: head h of row r of prompt b at
+ *              q + b * q_prompt + r * q_row + h * d (so a fused projection's rows are three pointers into it)
+ *   q_weight, k_weight  device [d] bf16, or NULL
+ *   cos_sin    device [table_rows][rot/2][2] f32: cosine and sine of every position's angles (may be NULL if rot = 0)
+ *   positions  device [B][rows] i32, or NULL for first + r.  A row whose position is not in the table gets NaN
+ *              in its rotated elements.
+ *   Qwin  device [B][L][H][W][d]: rows that are among the last W of the N positions (others are left as they are)
+ *   K, V  device [B][L][Hkv][N][d]: rows first .. first+rows-1 of layer `layer`
+ *   q_out device [B][rows][H][d], or NULL: all queries (for the layer's own attention)
+ * A decode step of all layers' tensors [B][L][H][d] and [B][L][Hkv][d] is the case N = W = rows = 1.  Inputs and
+ * outputs must not overlap.  dims.S is not used.  */
+SHOTKV_API int shotkv_norm_rope(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_rope* rope,
+                     const shotkv_bf16* q, const shotkv_bf16* k, const shotkv_bf16* v,
+                     const shotkv_bf16* q_weight, const shotkv_bf16* k_weight,
+                     const float* cos_sin, const int32_t* positions,
+                     shotkv_bf16* Qwin, shotkv_bf16* K, shotkv_bf16* V, shotkv_bf16* q_out, void* stream);
+
 /* ---- prefill (Algorithm 1, Phase 1) -------------------------------------------------------- */
 
 /* Window attention and column-sum: the alpha of the prefill score equation (Section 5.1).
@@ -273,6 +309,58 @@ SHOTKV_API int shotkv_decode_step_attend(shotkv_ctx* ctx, shotkv_decode_state* s
                        const shotkv_bf16* q, const shotkv_bf16* k_new, const shotkv_bf16* v_new,
                        const shotkv_bf16* Kc, const shotkv_bf16* Vc, const int32_t* kept_count,
                        float* attn_out, void* stream);
+
+/* ---- the compressed prompt in 4 bits --------------------------------------------------------- */
+
+/* Kc and Vc held in 4 bits an element.  An element is x = s * (c + z): a whole code c of -8..7, and a scale s and a whole
+ * z for its group -- 32 consecutive elements of a key, a value's whole row -- with
+ *   s      the least bf16 number that is no less than (max - min) / 15, max|x| / 240 and 2^-100 of the group,
+ *   c + z  = floor(x / s + 1/2),   z = 8 + the group's least such number.
+ * So an element is off by at most s / 2, every row stands by itself, and what is read is what is meant: s * (c + z) is
+ * exact in 32 bits.  A group with an element that is not finite, or whose range is beyond float32, reads as NaN.
+ * Keys and values of a unit (b, l, g) are ceil(Mcap / 32) tiles of 32 rows each, base addresses 16-byte aligned:
+ *   K4  device [B][L][Hkv][tiles][32 * (d/2 + d/8)] bytes      V4  device [B][L][Hkv][tiles][32 * (d/2 + 4)] bytes
+ * A tile is its codes as 32-bit words, then one word per group, row by row: s in the high half, z in the low half, both
+ * bf16.  Row r, dimension i of a tile: nibble n (bits 4n..4n+3, holding c + 8) of word ((r/16 * (d/64) + j/4) * 32 + lane) * 4 + j%4,
+ *   keys    lane = 4 (r%8) + i/8%4,       j = 2 (i/32) + i/4%2,     n = r/8%2 + 2 (i/2%2) + 4 (i%2)
+ *   values  lane = 4 (i/8%8) + r/2%4,     j = 4 (i/64) + i/2%4,     n = i%2 + 2 (r/8%2) + 4 (r%2)
+ * (the order in which the decode steps' matrix products take them).  */
+SHOTKV_API size_t shotkv_kv4_key_bytes(const shotkv_dims* dims, int32_t Mcap);    /* of K4, all units; 0 on invalid dims */
+SHOTKV_API size_t shotkv_kv4_value_bytes(const shotkv_dims* dims, int32_t Mcap);  /* of V4                               */
+
+/* shotkv_compact_kv into that form: row j of a unit is K's and V's row kept_idx[b][l][j], j < kept_count[b][l] (an index
+ * outside [0, N) gives a row of zeros).  kept_idx may be NULL: row j itself, to pack a cache that is compact already (Kc
+ * and Vc as K and V, N their rows).  Rows from kept_count to the end of the last tile that has kept rows become zeros;
+ * tiles beyond are left as they are.  dims: B, L, Hkv, d and N are used.  */
+SHOTKV_API int shotkv_compact_kv4(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_bf16* K, const shotkv_bf16* V,
+                       const int32_t* kept_idx, const int32_t* kept_count, int32_t Mcap, void* K4, void* V4,
+                       void* stream);
+
+/* The way back: Kc, Vc device [B][L][Hkv][Mcap][d], row j < kept_count[b][l] of every unit as s * (c + z) rounded to bf16 once.
+ * Rows from kept_count on are left as they are.  */
+SHOTKV_API int shotkv_unpack_kv4(shotkv_ctx* ctx, const shotkv_dims* dims, const void* K4, const void* V4,
+                      const int32_t* kept_count, int32_t Mcap, shotkv_bf16* Kc, shotkv_bf16* Vc, void* stream);
+
+/* shotkv_prefill_compress whose last step is shotkv_compact_kv4: all other arguments, outputs and codes are the same.  */
+SHOTKV_API int shotkv_prefill_compress_kv4(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_policy* policy,
+                                const shotkv_bf16* Qwin, const shotkv_bf16* K, const shotkv_bf16* V,
+                                const int32_t* offsets_host,
+                                float* shot_scores, uint8_t* keep, int32_t* kept_idx,
+                                int32_t* kept_count, int32_t Mcap, void* K4, void* V4,
+                                float* token_importance, uint32_t flags,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* shotkv_decode_step and shotkv_decode_step_attend with the compressed prompt in 4 bits (state->Mcap its rows, kept_count
+ * as there); the decode entries are bf16 as there, and state, eviction and outputs are the same.  A step may change from
+ * one form of the prompt to the other between calls.  Logits and outputs are sums in 32 bits over s * (c + z) as it
+ * stands: nothing is rounded on the way but the weights of the output, to 22 bits.  */
+SHOTKV_API int shotkv_decode_step_kv4(shotkv_ctx* ctx, shotkv_decode_state* state,
+                           const shotkv_bf16* q, const shotkv_bf16* k_new, const shotkv_bf16* v_new,
+                           const void* K4, const int32_t* kept_count, void* stream);
+SHOTKV_API int shotkv_decode_step_attend_kv4(shotkv_ctx* ctx, shotkv_decode_state* state,
+                                  const shotkv_bf16* q, const shotkv_bf16* k_new, const shotkv_bf16* v_new,
+                                  const void* K4, const void* V4, const int32_t* kept_count,
+                                  float* attn_out, void* stream);
 
 /* The work partition the scoring pass uses for `dims` on a GPU with `sm_count` SMs (host only; a
  * diagnostic and test aid).  Every prompt's keys [0, N) are cut into pieces at the shot boundaries

@@ -37,6 +37,8 @@ EXPORTS = [
     "shotkv_profile_enable", "shotkv_profile_read", "shotkv_launch_count", "shotkv_select_shots_static", "shotkv_plan_pieces",
     "shotkv_set_scoring_mode", "shotkv_repaired_items", "shotkv_set_pipeline_groups",
     "shotkv_set_wait_limit", "shotkv_selftest_bounded_wait", "shotkv_last_scoring_clock",
+    "shotkv_norm_rope", "shotkv_kv4_key_bytes", "shotkv_kv4_value_bytes", "shotkv_compact_kv4", "shotkv_unpack_kv4",
+    "shotkv_prefill_compress_kv4", "shotkv_decode_step_kv4", "shotkv_decode_step_attend_kv4",
 ]
 
 
@@ -60,6 +62,11 @@ class DecodeState(C.Structure):
                 ("T", C.c_int32), ("n_dec", C.c_int32),
                 ("Kd", C.c_void_p), ("Vd", C.c_void_p), ("acc", C.c_void_p), ("born", C.c_void_p),
                 ("ws", C.c_void_p), ("ws_bytes", C.c_size_t)]
+
+
+class Rope(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("layer", "first", "rows", "rot", "interleaved", "table_rows")] + [("eps", C.c_float)] +
+                [(n, C.c_int64) for n in ("q_row", "k_row", "v_row", "q_prompt", "k_prompt", "v_prompt")])
 
 
 _lib = None
@@ -107,6 +114,14 @@ def lib() -> C.CDLL:
         "shotkv_repaired_items": (C.c_uint64, [vp]),
         "shotkv_last_scoring_clock": (C.c_int, [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64)]),
         "shotkv_set_wait_limit": (C.c_int, [vp, C.c_int64]),
+        "shotkv_norm_rope": (C.c_int, [vp, PD, C.POINTER(Rope)] + [vp] * 12),
+        "shotkv_kv4_key_bytes": (sz, [PD, i32]),
+        "shotkv_kv4_value_bytes": (sz, [PD, i32]),
+        "shotkv_compact_kv4": (C.c_int, [vp, PD, vp, vp, vp, vp, i32, vp, vp, vp]),
+        "shotkv_unpack_kv4": (C.c_int, [vp, PD, vp, vp, vp, i32, vp, vp, vp]),
+        "shotkv_prefill_compress_kv4": (C.c_int, [vp, PD, PP, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, u32, vp, sz, vp]),
+        "shotkv_decode_step_kv4": (C.c_int, [vp, C.POINTER(DecodeState), vp, vp, vp, vp, vp, vp]),
+        "shotkv_decode_step_attend_kv4": (C.c_int, [vp, C.POINTER(DecodeState), vp, vp, vp, vp, vp, vp, vp, vp]),
         "shotkv_selftest_bounded_wait": (C.c_int, [vp, C.c_int64, C.POINTER(i32), vp]),
     }
     for name, (res, args) in sig.items():
@@ -114,9 +129,10 @@ def lib() -> C.CDLL:
         fn.restype, fn.argtypes = res, args
     m = _load_marshal()
     if m is not None:
-        m.init(Dims, Policy, DecodeState, *(C.cast(getattr(L, n), vp).value for n in (
+        m.init(Dims, Policy, DecodeState, Rope, *(C.cast(getattr(L, n), vp).value for n in (
             "shotkv_prefill_score", "shotkv_select_shots", "shotkv_compact_kv", "shotkv_prefill_compress",
-            "shotkv_decode_step", "shotkv_decode_step_attend")))
+            "shotkv_decode_step", "shotkv_decode_step_attend", "shotkv_norm_rope", "shotkv_compact_kv4", "shotkv_decode_step_kv4",
+            "shotkv_decode_step_attend_kv4")))
         _native = m
     _lib = L
     return L
@@ -431,6 +447,110 @@ def shotkv_decode_step_attend(ctx: Context, state: DecodeState, q, k_new, v_new,
     return ctx.check(rc)
 
 
+# ------------------------------------------------------------------ norm, rotation, layout; the prompt in 4 bits
+def make_rope(rows=1, rot=0, first=0, layer=0, interleaved=False, eps=1e-6) -> Rope:
+    """What shotkv_norm_rope does; it fills in the strides and the table's rows from the tensors it is given."""
+    return Rope(int(layer), int(first), int(rows), int(rot), int(bool(interleaved)), 0, float(eps))
+
+
+def _heads(t, rows, heads, d, B, name):
+    """Address, row stride and prompt stride of projected heads: a CUDA tensor [B, rows, heads, d] whose last two dimensions
+    are dense.  A stride of a dimension of one is of no consequence."""
+    if not (isinstance(t, torch.Tensor) and t.dtype is _BF16 and t.is_cuda):
+        _bad(t, _BF16, True, name)
+    if tuple(t.shape) != (B, rows, heads, d):
+        raise ValueError(f"{name}: expected shape {(B, rows, heads, d)}, got {tuple(t.shape)}")
+    sb, sr, sh, sd = t.stride()
+    if sd != 1 or (heads > 1 and sh != d):
+        raise ValueError(f"{name}: the heads of a row must be contiguous")
+    return t.data_ptr(), (sr if rows > 1 else 0), (sb if B > 1 else 0)
+
+
+def shotkv_norm_rope(ctx: Context, dims: Dims, rope: Rope, q, k, v, q_weight, k_weight, cos_sin, positions, Qwin, K, V, q_out=None,
+                     stream=None) -> int:
+    """q [B, rows, H, d], k and v [B, rows, Hkv, d] may be views of one projection; cos_sin [table rows, rot / 2, 2]."""
+    if _native is not None:
+        rc = _native.norm_rope(ctx._h, dims, rope, q, k, v, q_weight, k_weight, cos_sin, positions, Qwin, K, V, q_out, stream)
+        if rc is not None:
+            return ctx.check(rc)
+    qp, rope.q_row, rope.q_prompt = _heads(q, rope.rows, dims.H, dims.d, dims.B, "q")
+    kp, rope.k_row, rope.k_prompt = _heads(k, rope.rows, dims.Hkv, dims.d, dims.B, "k")
+    vp, rope.v_row, rope.v_prompt = _heads(v, rope.rows, dims.Hkv, dims.d, dims.B, "v")
+    if cos_sin is not None and tuple(cos_sin.shape[1:]) != (rope.rot // 2, 2):
+        raise ValueError(f"cos_sin: expected shape [rows, {rope.rot // 2}, 2], got {tuple(cos_sin.shape)}")
+    rope.table_rows = 0 if cos_sin is None else cos_sin.shape[0]
+    rc = lib().shotkv_norm_rope(ctx._h, C.byref(dims), C.byref(rope), qp, kp, vp, _dev(q_weight, _BF16, "q_weight"),
+                                _dev(k_weight, _BF16, "k_weight"), _dev(cos_sin, _F32, "cos_sin"), _dev(positions, _I32, "positions"),
+                                _dev(Qwin, _BF16, "Qwin"), _dev(K, _BF16, "K"), _dev(V, _BF16, "V"), _dev(q_out, _BF16, "q_out"),
+                                _stream(stream))
+    return ctx.check(rc)
+
+
+def shotkv_kv4_key_bytes(dims: Dims, Mcap: int) -> int:
+    return int(lib().shotkv_kv4_key_bytes(C.byref(dims), int(Mcap)))
+
+
+def shotkv_kv4_value_bytes(dims: Dims, Mcap: int) -> int:
+    return int(lib().shotkv_kv4_value_bytes(C.byref(dims), int(Mcap)))
+
+
+def alloc_kv4(dims: Dims, Mcap: int, device="cuda"):
+    """Allocates (does not compute) K4 and V4 [B, L, Hkv, tiles, bytes of a tile], uint8, for Mcap rows a unit."""
+    tiles, units = (int(Mcap) + 31) // 32, dims.B * dims.L * dims.Hkv
+    return tuple(torch.zeros(dims.B, dims.L, dims.Hkv, tiles, n // (units * tiles), dtype=torch.uint8, device=device)
+                 for n in (shotkv_kv4_key_bytes(dims, Mcap), shotkv_kv4_value_bytes(dims, Mcap)))
+
+
+def shotkv_compact_kv4(ctx: Context, dims: Dims, K, V, kept_idx, kept_count, Mcap: int, K4, V4, stream=None) -> int:
+    if _native is not None:
+        rc = _native.compact_kv4(ctx._h, dims, K, V, kept_idx, kept_count, Mcap, K4, V4, stream)
+        if rc is not None:
+            return ctx.check(rc)
+    rc = lib().shotkv_compact_kv4(ctx._h, C.byref(dims), _dev(K, _BF16, "K"), _dev(V, _BF16, "V"), _dev(kept_idx, _I32, "kept_idx"),
+                                  _dev(kept_count, _I32, "kept_count"), int(Mcap), _dev(K4, _U8, "K4"), _dev(V4, _U8, "V4"),
+                                  _stream(stream))
+    return ctx.check(rc)
+
+
+def shotkv_unpack_kv4(ctx: Context, dims: Dims, K4, V4, kept_count, Mcap: int, Kc, Vc, stream=None) -> int:
+    rc = lib().shotkv_unpack_kv4(ctx._h, C.byref(dims), _dev(K4, _U8, "K4"), _dev(V4, _U8, "V4"), _dev(kept_count, _I32, "kept_count"),
+                                 int(Mcap), _dev(Kc, _BF16, "Kc"), _dev(Vc, _BF16, "Vc"), _stream(stream))
+    return ctx.check(rc)
+
+
+def shotkv_prefill_compress_kv4(ctx: Context, dims: Dims, policy: Policy, Qwin, K, V, offsets, shot_scores, keep, kept_idx, kept_count,
+                                Mcap: int, K4, V4, token_importance, flags: int, ws, stream=None) -> int:
+    o = _offsets(offsets)
+    rc = lib().shotkv_prefill_compress_kv4(
+        ctx._h, C.byref(dims), C.byref(policy), _dev(Qwin, _BF16, "Qwin"), _dev(K, _BF16, "K"), _dev(V, _BF16, "V"), o.ctypes.data,
+        _dev(shot_scores, _F32, "shot_scores"), _dev(keep, _U8, "keep"), _dev(kept_idx, _I32, "kept_idx"),
+        _dev(kept_count, _I32, "kept_count"), int(Mcap), _dev(K4, _U8, "K4"), _dev(V4, _U8, "V4"),
+        _dev(token_importance, _F32, "token_importance"), int(flags), *_raw(ws, "ws"), _stream(stream))
+    return ctx.check(rc)
+
+
+def shotkv_decode_step_kv4(ctx: Context, state: DecodeState, q, k_new, v_new, K4, kept_count, stream=None) -> int:
+    if _native is not None:
+        rc = _native.decode_step_kv4(ctx._h, state, q, k_new, v_new, K4, kept_count, stream)
+        if rc is not None:
+            return ctx.check(rc)
+    rc = lib().shotkv_decode_step_kv4(ctx._h, C.byref(state), _dev(q, _BF16, "q"), _dev(k_new, _BF16, "k_new"),
+                                      _dev(v_new, _BF16, "v_new"), _dev(K4, _U8, "K4"), _dev(kept_count, _I32, "kept_count"),
+                                      _stream(stream))
+    return ctx.check(rc)
+
+
+def shotkv_decode_step_attend_kv4(ctx: Context, state: DecodeState, q, k_new, v_new, K4, V4, kept_count, attn_out, stream=None) -> int:
+    if _native is not None:
+        rc = _native.decode_step_attend_kv4(ctx._h, state, q, k_new, v_new, K4, V4, kept_count, attn_out, stream)
+        if rc is not None:
+            return ctx.check(rc)
+    rc = lib().shotkv_decode_step_attend_kv4(ctx._h, C.byref(state), _dev(q, _BF16, "q"), _dev(k_new, _BF16, "k_new"),
+                                             _dev(v_new, _BF16, "v_new"), _dev(K4, _U8, "K4"), _dev(V4, _U8, "V4"),
+                                             _dev(kept_count, _I32, "kept_count"), _dev(attn_out, _F32, "attn_out"), _stream(stream))
+    return ctx.check(rc)
+
+
 def shotkv_plan_pieces(dims: Dims, offsets=None, sm_count: int = 148):
     """(nchunk, chunk_keys, pieces [B][P][3]) of the scoring pass's work partition (host only)."""
     o = _offsets(offsets) if offsets is not None else None
@@ -509,7 +629,8 @@ def alloc_prefill_outputs(dims: Dims, Mcap: int, device="cuda", token_importance
 
 
 __all__ = [n for n in dir() if n.startswith("shotkv_")] + [
-    "Context", "Dims", "Policy", "DecodeState", "ShotKVError", "make_dims", "per_head_dims", "make_policy", "alloc_prefill_outputs",
+    "Context", "Dims", "Policy", "DecodeState", "Rope", "ShotKVError", "make_dims", "per_head_dims", "make_policy", "make_rope",
+    "alloc_prefill_outputs", "alloc_kv4",
     "OK", "ERR_INVALID_ARG", "ERR_UNSUPPORTED_SHAPE", "ERR_BAD_OFFSETS", "ERR_WORKSPACE_TOO_SMALL", "ERR_CUDA",
     "ERR_TIMEOUT", "WARN_BUDGET_BELOW_ALWAYS_KEPT", "FLAG_TOKEN_IMPORTANCE", "EXPORTS", "LIB_PATH", "lib",
     "SCORING_FAST", "SCORING_EXACT", "shotkv_set_scoring_mode", "shotkv_repaired_items", "shotkv_set_pipeline_groups",

@@ -507,6 +507,106 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&v);
 }
 
+// Where a CTA stands: its unit, the unit's (sequence, layer) and KV head, its number among the unit's CTAs; in the cluster the unit's
+// first CTA, and how many there are of the (sequence, layer).
+struct UnitPart { int u, bl, hk, rank, first_cta, ctas; };
+// A group's output rows are handed round in quads of four elements: quad q is added up by CTA q % nsplit, as its
+// quad number q / nsplit (256 quads and 16 CTAs at most: the product with `over` / 65536 is exact).
+struct QuadShare { int quads, over, share, owned; };
+template <int D>
+__device__ __forceinline__ QuadShare quads_of(int G, int nsplit, int rank) {
+    QuadShare s;
+    s.quads = G * (D / 4), s.over = 65536 / nsplit + 1;
+    s.share = (s.quads * s.over) >> 16, s.owned = s.share + (rank < s.quads - s.share * nsplit);
+    return s;
+}
+template <int D>
+constexpr int kOutPitch = D + 4;                           // floats a row of a warp's outputs
+
+// The end of a fused step in a CTA of NW warps, by all its threads after a barrier.  Shared memory: (m, z) of the warps' 8
+// rows in `sred`, the warps' outputs [8 rows][kOutPitch] in `sO`, `pitch` floats apart, logits of the decode entries in `sdec`;
+// of a cluster: `stab` [nsplit][8 rows] (m, z) of its CTAs, `sin` [nsplit][share + 1] their outputs, of which this CTA has
+// its share of the quads, and the barrier of what they send here.  `begin`: of a shared unit, the first decode entry among
+// this warp's blocks of 16.
+template <int D, int NW, bool FUSED>
+__device__ __forceinline__ void finish_attend(const DecodeParams& p, const DecodeFinishParams& f, const UnitPart& part, const QuadShare& qs,
+                                              const FusedEnd& end, float2* sred, float* sdec, float2* stab, float4* sin,
+                                              unsigned long long* arrived, const float* sO, int pitch, int begin) {
+    constexpr int NT = NW * 32;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3;
+    const int quads = qs.quads, over = qs.over, share = qs.share, owned = qs.owned;
+    float* out = p.out + ((size_t)part.bl * p.H + (size_t)part.hk * p.G) * D;
+    if (p.nsplit > 1 && tid < 8 * p.nsplit) {                // every CTA's rows to every CTA
+        float fac[NW];
+        send(stab + part.rank * 8 + (tid & 7), part.first_cta + (tid >> 3), arrived, row_of_cta(sred, tid & 7, fac));
+    }
+    // the warps' outputs relative to the CTA's maximum: alone, the CTA has the rows' whole sums
+#pragma unroll 1
+    for (int q = tid; q < quads; q += NT) {
+        const int r = q / (D / 4), c = q % (D / 4) * 4;
+        float fac[NW];
+        const float2 row = row_of_cta(sred, r, fac);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float4 v = *reinterpret_cast<const float4*>(sO + w * pitch + r * kOutPitch<D> + c);
+            if (fac[w] >= 0.f) o.x += v.x * fac[w], o.y += v.y * fac[w], o.z += v.z * fac[w], o.w += v.w * fac[w];
+        }
+        if (p.nsplit > 1) {
+            const int slot = (q * over) >> 16, to = q - slot * p.nsplit;
+            send(sin + part.rank * (share + 1) + slot, part.first_cta + to, arrived, o);
+        } else {
+            const float iz = row.y > 0.f ? 1.f / row.y : 0.f;
+            float* d = out + 4 * q;
+            d[0] = o.x * iz;
+            d[1] = o.y * iz;
+            d[2] = o.z * iz;
+            d[3] = o.w * iz;
+        }
+    }
+    const bool ok = p.nsplit <= 1 || await_messages(arrived, p.err, p.wait_cycles);
+    float rm, riz;                                           // of row lane / 4, over all keys of the unit
+    row_of_unit(p.nsplit > 1 ? stab : sred, p.nsplit > 1 ? p.nsplit : NW, rm, riz);
+    const float rmu = rm == SHOTKV_NEG_INF ? 0.f : rm;
+    // the CTA's own quads, four lanes each of which adds up every fourth CTA's
+    if (p.nsplit > 1) {
+#pragma unroll 1
+        for (int x = tid; x < (owned * 4 + 31) / 32 * 32; x += NT) {
+            const int slot = x >> 2, q = slot * p.nsplit + part.rank;
+            const int r = slot < owned ? q / (D / 4) : 0;
+            const float mu = __shfl_sync(0xffffffffu, rmu, r * 4), iz = __shfl_sync(0xffffffffu, riz, r * 4);
+            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < kMaxSplit / 4; ++i) {
+                const int c = t4 + 4 * i;
+                if (slot < owned && c < p.nsplit) {
+                    const float4 v = sin[c * (share + 1) + slot];
+                    const float e = ex2f(stab[c * 8 + r].x - mu);
+                    o.x += v.x * e, o.y += v.y * e, o.z += v.z * e, o.w += v.w * e;
+                }
+            }
+#pragma unroll
+            for (int d = 1; d <= 2; d <<= 1) {
+                o.x += __shfl_xor_sync(0xffffffffu, o.x, d);
+                o.y += __shfl_xor_sync(0xffffffffu, o.y, d);
+                o.z += __shfl_xor_sync(0xffffffffu, o.z, d);
+                o.w += __shfl_xor_sync(0xffffffffu, o.w, d);
+            }
+            if (slot < owned) out[4 * q + t4] = (t4 == 0 ? o.x : t4 == 1 ? o.y : t4 == 2 ? o.z : o.w) * iz;
+        }
+    }
+    // the decode entries, their weights summed over the query rows: of a shared unit those among this warp's blocks, 16 lanes
+    // at a time; whole units have them all here, and a lane each (768 units of 608 keys and 390 decode entries, d = 64: 46.3
+    // -> 43.2 us a step, eight query heads to a KV head 50.8 -> 45.7)
+    const bool whole = p.nsplit == 1;
+    entry_weights(sdec, p.Dcap, p.G, rm, riz, whole ? warp * 32 : begin, f.n, whole ? NT : p.nsplit * NW * 16, whole ? 32 : 16, [&](int j, float s) {
+        if (FUSED) fused_send(end, f, part.hk, j, s, part.ctas);
+        else p.partial[(size_t)part.u * p.Dcap + j] = s;
+    });
+    const bool all = !FUSED || fused_finish<D, NT>(end, f, part.bl, part.first_cta + part.rank, part.ctas, p);
+    if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err, p.wait_cycles);
+}
+
 // Shared-memory staging of the fused step: every warp owns a ring of kStages stages, a stage
 // holding the 16 key rows and the 16 value rows of one block, unpadded, with the 16-byte chunks of a
 // row permuted so that the reads are free of bank conflicts: keys (read back as 16 bytes per lane,
@@ -520,8 +620,7 @@ struct AttendCfg {
     static constexpr int kTileBytes = 16 * kRowBytes;             // 16 rows of keys (or of values)
     static constexpr int kStageBytes = 2 * kTileBytes;
     static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
-    static constexpr int kOutPitch = D + 4;                       // floats a row of a warp's outputs
-    static_assert(8 * kOutPitch * 4 <= kStages * kStageBytes, "a warp's outputs take the place of its ring");
+    static_assert(8 * kOutPitch<D> * 4 <= kStages * kStageBytes, "a warp's outputs take the place of its ring");
 };
 
 // Dynamic shared memory of the decode kernels for decode regions of Dcap rows, multiples of 16 bytes.
@@ -569,14 +668,12 @@ __global__ void __launch_bounds__(AttendCfg<D>::kWarps * 32, 3) decode_attend_ke
     constexpr int NB = D / 32;     // 32-dim blocks
     constexpr int VPR = D / 8;     // 16-byte chunks per row
     constexpr int MT = D / 16;     // 16-dim tiles of the output
-    constexpr int NW = Cfg::kWarps, NS = Cfg::kStages, NT = NW * 32;
+    constexpr int NW = Cfg::kWarps, NS = Cfg::kStages;
     extern __shared__ __align__(128) unsigned char dsm[];
     // [NW][NS][keys | values][16 rows][D bf16]; later each warp's outputs [8 rows][PITCH]
     unsigned char* ring = dsm;
     float2* sred = reinterpret_cast<float2*>(ring + Cfg::kRingBytes + 16);   // [NW warps][8 rows]  (m, z)
     float* sdec = reinterpret_cast<float*>(sred + NW * 8);   // [G][Dcap]  logits of the decode entries
-    // of a cluster: [nsplit][8 rows] (m, z) of its CTAs, [nsplit][share] their outputs, of which this CTA has its share of the
-    // quads, and the barrier of what they send here
     float2* stab = reinterpret_cast<float2*>(sdec + ((p.G * p.Dcap + 3) & ~3));
     float4* sin = reinterpret_cast<float4*>(stab + p.nsplit * 8);
     unsigned long long* arrived = reinterpret_cast<unsigned long long*>(sred) - 1;
@@ -584,17 +681,14 @@ __global__ void __launch_bounds__(AttendCfg<D>::kWarps * 32, 3) decode_attend_ke
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, t4 = lane & 3;
     const int u = blockIdx.x / p.nsplit, rank = blockIdx.x - u * p.nsplit;
-    // The group's output rows are handed round in quads of four elements: quad q is added up by CTA q % nsplit, as its
-    // quad number q / nsplit (256 quads and 16 CTAs at most: the product is exact).
-    const int quads = p.G * (D / 4), over = 65536 / p.nsplit + 1;
-    const int share = (quads * over) >> 16, owned = share + (rank < quads - share * p.nsplit);
+    const QuadShare qs = quads_of<D>(p.G, p.nsplit, rank);
     const int bl = u / p.Hkv, hk = u - bl * p.Hkv;
     const int first_cta = FUSED ? hk * p.nsplit : 0, ctas = p.Hkv * p.nsplit;   // in the cluster: the unit's first; FUSED: all
     FusedEnd end{};
     if (FUSED) end = fused_end_at(dsm + attend_smem_bytes<D>(p.G, p.Dcap, p.nsplit), f);
     if (FUSED || p.nsplit > 1) {
         if (tid == 0) {
-            if (p.nsplit > 1) expect_messages(arrived, p.nsplit * (8 * (int)sizeof(float2) + owned * (int)sizeof(float4)));
+            if (p.nsplit > 1) expect_messages(arrived, p.nsplit * (8 * (int)sizeof(float2) + qs.owned * (int)sizeof(float4)));
             if (FUSED) fused_expect(end, f, first_cta + rank);
         }
         cluster_arrive();
@@ -777,7 +871,7 @@ __global__ void __launch_bounds__(AttendCfg<D>::kWarps * 32, 3) decode_attend_ke
     z += __shfl_xor_sync(0xffffffffu, z, 2);
     if (t4 == 0) sred[warp * 8 + g] = make_float2(m, z);
     __syncwarp();                                           // all lanes are done with the warp's ring: its outputs take its place
-    constexpr int PITCH = Cfg::kOutPitch, kWarpRing = NS * Cfg::kStageBytes / 4;    // floats
+    constexpr int PITCH = kOutPitch<D>, kWarpRing = NS * Cfg::kStageBytes / 4;    // floats
     float* sO = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
@@ -788,77 +882,8 @@ __global__ void __launch_bounds__(AttendCfg<D>::kWarps * 32, 3) decode_attend_ke
         o[PITCH + 8] = O[mt][3];
     }
     __syncthreads();
-    float* out = p.out + ((size_t)bl * p.H + (size_t)hk * p.G) * D;
-    if (p.nsplit > 1 && tid < 8 * p.nsplit) {                // every CTA's rows to every CTA
-        float fac[NW];
-        send(stab + rank * 8 + (tid & 7), first_cta + (tid >> 3), arrived, row_of_cta(sred, tid & 7, fac));
-    }
-    // the warps' outputs relative to the CTA's maximum: alone, the CTA has the rows' whole sums
-#pragma unroll 1
-    for (int q = tid; q < quads; q += NT) {
-        const int r = q / (D / 4), c = q % (D / 4) * 4;
-        float fac[NW];
-        const float2 row = row_of_cta(sred, r, fac);
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float4 v = *reinterpret_cast<const float4*>(sO + w * kWarpRing + r * PITCH + c);
-            if (fac[w] >= 0.f) o.x += v.x * fac[w], o.y += v.y * fac[w], o.z += v.z * fac[w], o.w += v.w * fac[w];
-        }
-        if (p.nsplit > 1) {
-            const int slot = (q * over) >> 16, to = q - slot * p.nsplit;
-            send(sin + rank * (share + 1) + slot, first_cta + to, arrived, o);
-        } else {
-            const float iz = row.y > 0.f ? 1.f / row.y : 0.f;
-            float* d = out + 4 * q;
-            d[0] = o.x * iz;
-            d[1] = o.y * iz;
-            d[2] = o.z * iz;
-            d[3] = o.w * iz;
-        }
-    }
-    const bool ok = p.nsplit <= 1 || await_messages(arrived, p.err, p.wait_cycles);
-    float rm, riz;                                           // of row lane / 4, over all keys of the unit
-    row_of_unit(p.nsplit > 1 ? stab : sred, p.nsplit > 1 ? p.nsplit : NW, rm, riz);
-    const float rmu = rm == SHOTKV_NEG_INF ? 0.f : rm;
-    // the CTA's own quads, four lanes each of which adds up every fourth CTA's
-    if (p.nsplit > 1) {
-#pragma unroll 1
-        for (int x = tid; x < (owned * 4 + 31) / 32 * 32; x += NT) {
-            const int slot = x >> 2, q = slot * p.nsplit + rank;
-            const int r = slot < owned ? q / (D / 4) : 0;
-            const float mu = __shfl_sync(0xffffffffu, rmu, r * 4), iz = __shfl_sync(0xffffffffu, riz, r * 4);
-            float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int i = 0; i < kMaxSplit / 4; ++i) {
-                const int c = t4 + 4 * i;
-                if (slot < owned && c < p.nsplit) {
-                    const float4 v = sin[c * (share + 1) + slot];
-                    const float e = ex2f(stab[c * 8 + r].x - mu);
-                    o.x += v.x * e, o.y += v.y * e, o.z += v.z * e, o.w += v.w * e;
-                }
-            }
-#pragma unroll
-            for (int d = 1; d <= 2; d <<= 1) {
-                o.x += __shfl_xor_sync(0xffffffffu, o.x, d);
-                o.y += __shfl_xor_sync(0xffffffffu, o.y, d);
-                o.z += __shfl_xor_sync(0xffffffffu, o.z, d);
-                o.w += __shfl_xor_sync(0xffffffffu, o.w, d);
-            }
-            if (slot < owned) out[4 * q + t4] = (t4 == 0 ? o.x : t4 == 1 ? o.y : t4 == 2 ? o.z : o.w) * iz;
-        }
-    }
-    // the decode entries, their weights summed over the query rows: of a shared unit those among this warp's blocks, 16 lanes
-    // at a time; whole units have them all here, and a lane each (768 units of 608 keys and 390 decode entries, d = 64: 46.3
-    // -> 43.2 us a step, eight query heads to a KV head 50.8 -> 45.7)
-    const bool whole = p.nsplit == 1;
-    const int begin = whole ? warp * 32 : first + max(0, (M - 15 - first + STRIDE - 1) / STRIDE) * STRIDE - M;
-    entry_weights(sdec, p.Dcap, p.G, rm, riz, begin, n, whole ? NT : STRIDE, whole ? 32 : 16, [&](int j, float s) {
-        if (FUSED) fused_send(end, f, hk, j, s, ctas);
-        else p.partial[(size_t)u * p.Dcap + j] = s;
-    });
-    const bool all = !FUSED || fused_finish<D, NT>(end, f, bl, first_cta + rank, ctas, p);
-    if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err, p.wait_cycles);
+    finish_attend<D, NW, FUSED>(p, f, UnitPart{u, bl, hk, rank, first_cta, ctas}, qs, end, sred, sdec, stab, sin, arrived, sO, kWarpRing,
+                                first + max(0, (M - 15 - first + STRIDE - 1) / STRIDE) * STRIDE - M);
 }
 
 }  // namespace shotkv

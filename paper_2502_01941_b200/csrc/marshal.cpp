@@ -17,13 +17,17 @@
 
 namespace {
 
-PyTypeObject *g_dims, *g_policy, *g_state;      // the ctypes structures of binding.py
+PyTypeObject *g_dims, *g_policy, *g_state, *g_rope;      // the ctypes structures of binding.py
 decltype(&shotkv_prefill_score) g_prefill_score;
 decltype(&shotkv_select_shots) g_select_shots;
 decltype(&shotkv_compact_kv) g_compact_kv;
 decltype(&shotkv_prefill_compress) g_prefill_compress;
 decltype(&shotkv_decode_step) g_decode_step;
 decltype(&shotkv_decode_step_attend) g_decode_step_attend;
+decltype(&shotkv_norm_rope) g_norm_rope;
+decltype(&shotkv_compact_kv4) g_compact_kv4;
+decltype(&shotkv_decode_step_kv4) g_decode_step_kv4;
+decltype(&shotkv_decode_step_attend_kv4) g_decode_step_attend_kv4;
 
 // Reads one argument after the other; `ok` falls when one is not as expected, and the rest is not read.
 struct Args {
@@ -86,6 +90,38 @@ struct Args {
     float* f32() { return tensor<float>(at::kFloat); }
     int32_t* i32() { return tensor<int32_t>(at::kInt); }
     uint8_t* u8() { return tensor<uint8_t>(at::kByte); }
+    // projected heads [B][rows][heads][d], the last two dimensions dense
+    const shotkv_bf16* heads(const shotkv_dims* dims, int rows, int heads, int64_t& row, int64_t& prompt) {
+        PyObject* o = next();
+        if (!ok || !THPVariable_CheckExact(o)) {
+            ok = false;
+            return nullptr;
+        }
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (!t.is_cuda() || t.layout() != at::kStrided || t.scalar_type() != at::kBFloat16 || t.dim() != 4 || t.size(0) != dims->B ||
+            t.size(1) != rows || t.size(2) != heads || t.size(3) != dims->d || t.stride(3) != 1 || (heads > 1 && t.stride(2) != dims->d)) {
+            ok = false;
+            return nullptr;
+        }
+        row = rows > 1 ? t.stride(1) : 0;
+        prompt = dims->B > 1 ? t.stride(0) : 0;
+        return static_cast<const shotkv_bf16*>(t.data_ptr());
+    }
+    // [table rows][rot / 2][2], or None
+    const float* table(shotkv_rope* r) {
+        if (ok && i < n && a[i] == Py_None) {
+            ++i;
+            r->table_rows = 0;
+            return nullptr;
+        }
+        const at::Tensor* t = cuda_tensor();
+        if (!ok || t->scalar_type() != at::kFloat || t->dim() != 3 || t->size(1) != r->rot / 2 || t->size(2) != 2 || t->size(0) > INT32_MAX) {
+            ok = false;
+            return nullptr;
+        }
+        r->table_rows = (int32_t)t->size(0);
+        return static_cast<const float*>(t->data_ptr());
+    }
     void* raw(size_t& bytes) {
         const at::Tensor* t = cuda_tensor();
         if (!ok) return nullptr;
@@ -232,19 +268,75 @@ PyObject* decode_step_attend(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// init(Dims, Policy, DecodeState, addresses of the six functions in the order above)
+PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, [](Args& g) {
+        auto* c = g.context();
+        auto* d = g.structure<shotkv_dims>(g_dims);
+        auto* r = g.structure<shotkv_rope>(g_rope);
+        const shotkv_bf16 *q = nullptr, *k = nullptr, *v = nullptr;
+        if (g.ok) q = g.heads(d, r->rows, d->H, r->q_row, r->q_prompt);
+        if (g.ok) k = g.heads(d, r->rows, d->Hkv, r->k_row, r->k_prompt);
+        if (g.ok) v = g.heads(d, r->rows, d->Hkv, r->v_row, r->v_prompt);
+        auto *qw = g.bf16(), *kw = g.bf16();
+        const float* cs = g.ok ? g.table(r) : nullptr;
+        auto* pos = g.i32();
+        auto *Q = g.bf16(), *K = g.bf16(), *V = g.bf16(), *qo = g.bf16();
+        void* st = g.stream();
+        return [=] { return g_norm_rope(c, d, r, q, k, v, qw, kw, cs, pos, Q, K, V, qo, st); };
+    });
+}
+PyObject* compact_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, [](Args& g) {
+        auto* c = g.context();
+        auto* d = g.structure<shotkv_dims>(g_dims);
+        auto *K = g.bf16(), *V = g.bf16();
+        auto *idx = g.i32(), *count = g.i32();
+        const int32_t mcap = (int32_t)g.integer(INT32_MIN, INT32_MAX);
+        auto *K4 = g.u8(), *V4 = g.u8();
+        void* st = g.stream();
+        return [=] { return g_compact_kv4(c, d, K, V, idx, count, mcap, K4, V4, st); };
+    });
+}
+PyObject* decode_step_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, [](Args& g) {
+        auto* c = g.context();
+        auto* s = g.structure<shotkv_decode_state>(g_state);
+        auto *q = g.bf16(), *k = g.bf16(), *v = g.bf16();
+        auto* K4 = g.u8();
+        auto* count = g.i32();
+        void* st = g.stream();
+        return [=] { return g_decode_step_kv4(c, s, q, k, v, K4, count, st); };
+    });
+}
+PyObject* decode_step_attend_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, [](Args& g) {
+        auto* c = g.context();
+        auto* s = g.structure<shotkv_decode_state>(g_state);
+        auto *q = g.bf16(), *k = g.bf16(), *v = g.bf16();
+        auto *K4 = g.u8(), *V4 = g.u8();
+        auto* count = g.i32();
+        auto* out = g.f32();
+        void* st = g.stream();
+        return [=] { return g_decode_step_attend_kv4(c, s, q, k, v, K4, V4, count, out, st); };
+    });
+}
+
+// init(Dims, Policy, DecodeState, Rope, addresses of the ten functions in the order above)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 9 || !PyType_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2])) {
-        PyErr_SetString(PyExc_TypeError, "init(Dims, Policy, DecodeState, six addresses)");
+    constexpr int kTypes = 4, kFunctions = 10;
+    bool ok = n == kTypes + kFunctions;
+    for (int k = 0; ok && k < kTypes; ++k) ok = PyType_Check(a[k]);
+    if (!ok) {
+        PyErr_SetString(PyExc_TypeError, "init(Dims, Policy, DecodeState, Rope, ten addresses)");
         return nullptr;
     }
-    void* f[6];
-    for (int k = 0; k < 6; ++k) {
-        f[k] = PyLong_AsVoidPtr(a[3 + k]);
+    void* f[kFunctions];
+    for (int k = 0; k < kFunctions; ++k) {
+        f[k] = PyLong_AsVoidPtr(a[kTypes + k]);
         if (PyErr_Occurred()) return nullptr;
     }
-    PyTypeObject** types[3] = {&g_dims, &g_policy, &g_state};
-    for (int k = 0; k < 3; ++k) {
+    PyTypeObject** types[kTypes] = {&g_dims, &g_policy, &g_state, &g_rope};
+    for (int k = 0; k < kTypes; ++k) {
         Py_INCREF(a[k]);
         Py_XDECREF(reinterpret_cast<PyObject*>(*types[k]));
         *types[k] = reinterpret_cast<PyTypeObject*>(a[k]);
@@ -255,12 +347,17 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_prefill_compress = reinterpret_cast<decltype(g_prefill_compress)>(f[3]);
     g_decode_step = reinterpret_cast<decltype(g_decode_step)>(f[4]);
     g_decode_step_attend = reinterpret_cast<decltype(g_decode_step_attend)>(f[5]);
+    g_norm_rope = reinterpret_cast<decltype(g_norm_rope)>(f[6]);
+    g_compact_kv4 = reinterpret_cast<decltype(g_compact_kv4)>(f[7]);
+    g_decode_step_kv4 = reinterpret_cast<decltype(g_decode_step_kv4)>(f[8]);
+    g_decode_step_attend_kv4 = reinterpret_cast<decltype(g_decode_step_attend_kv4)>(f[9]);
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(init), FAST(prefill_score), FAST(select_shots), FAST(compact_kv), FAST(prefill_compress),
-                           FAST(decode_step), FAST(decode_step_attend), {nullptr, nullptr, 0, nullptr}};
+                           FAST(decode_step), FAST(decode_step_attend), FAST(norm_rope), FAST(compact_kv4),
+                           FAST(decode_step_kv4), FAST(decode_step_attend_kv4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods};
 
 }  // namespace

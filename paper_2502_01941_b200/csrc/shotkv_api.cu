@@ -20,6 +20,9 @@
 #include "colsum_tc.cuh"
 #include "common.cuh"
 #include "decode.cuh"
+#include "decode_kv4.cuh"
+#include "kv4.cuh"
+#include "norm_rope.cuh"
 #include "score_fast.cuh"
 #include "score_stream.cuh"
 #include "reductions.cuh"
@@ -106,6 +109,7 @@ struct shotkv_ctx {
     int32_t* static_offsets = nullptr;         // device address of the built-in boundary table (looked up on first use)
     void* encode_tiled = nullptr;              // cuTensorMapEncodeTiled, resolved at creation
     DecodeRoom room_attend[2][2], room_score[2][2];   // [d = 128][the step ends in its first kernel] (asked at creation)
+    DecodeRoom room_kv4[2][2][2];              // [d = 128][with the attention output][the step ends in its first kernel]
     int whole_score[2][2] = {};                // CTAs that have a unit each and fit an SM, two and four blocks of keys deep
 };
 
@@ -748,6 +752,33 @@ int run_compact(shotkv_ctx* ctx, const shotkv_dims* d, const shotkv_bf16* K, con
                   kept_idx, kept_count, (int)d->Hkv, (int)d->N, (int)Mcap, (uint4*)Kc, (uint4*)Vc);
 }
 
+// The same into 4 bits: a warp per 16 rows.
+int run_compact_kv4(shotkv_ctx* ctx, const shotkv_dims* d, const shotkv_bf16* K, const shotkv_bf16* V, const int32_t* kept_idx,
+                    const int32_t* kept_count, int32_t Mcap, void* K4, void* V4, cudaStream_t stream) {
+    const dim3 grid((2 * kv4_tiles(Mcap) + kPackThreads / 32 - 1) / (kPackThreads / 32), d->Hkv, d->B * d->L);
+    if (grid.y > 65535 || grid.z > 65535) return fail(ctx, SHOTKV_ERR_UNSUPPORTED_SHAPE, "Hkv and B*L must be <= 65535");
+    return launch(ctx, d->d == 128 ? compact_kv4_kernel<128> : compact_kv4_kernel<64>, grid, kPackThreads, 0, stream, 1, kEarly, (const uint4*)K,
+                  (const uint4*)V, kept_idx, kept_count, (int)d->Hkv, (int)d->N, (int)Mcap, (unsigned char*)K4, (unsigned char*)V4);
+}
+
+// Where the kept rows go: bf16 rows, or packed tiles.
+struct KeptRows {
+    void *K, *V;
+    bool packed;
+};
+size_t kv4_unit_bytes(const shotkv_dims* d, int32_t Mcap, bool values) {
+    const int tile = d->d == 128 ? (values ? Kv4<128>::kValueTile : Kv4<128>::kKeyTile) : (values ? Kv4<64>::kValueTile : Kv4<64>::kKeyTile);
+    return (size_t)kv4_tiles(Mcap) * tile;
+}
+int run_keep(shotkv_ctx* ctx, const shotkv_dims* d, const shotkv_bf16* K, const shotkv_bf16* V, const int32_t* kept_idx,
+             const int32_t* kept_count, int32_t Mcap, const KeptRows& to, size_t unit, cudaStream_t stream) {
+    if (to.packed)
+        return run_compact_kv4(ctx, d, K, V, kept_idx, kept_count, Mcap, (unsigned char*)to.K + unit * kv4_unit_bytes(d, Mcap, false),
+                               (unsigned char*)to.V + unit * kv4_unit_bytes(d, Mcap, true), stream);
+    const size_t at = unit * (size_t)Mcap * d->d;
+    return run_compact(ctx, d, K, V, kept_idx, kept_count, Mcap, (shotkv_bf16*)to.K + at, (shotkv_bf16*)to.V + at, stream);
+}
+
 // Dynamic shared-memory limits of every kernel that may need more than the 48 KB default.  A
 // function attribute belongs to the device's context, so it is set once when a shotkv_ctx is
 // created on that device, never on a launch path.
@@ -796,10 +827,17 @@ cudaError_t set_kernel_attributes() {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     };
+    const void* kv4[] = {(const void*)decode_kv4_kernel<128, true, false>,  (const void*)decode_kv4_kernel<128, true, true>,
+                         (const void*)decode_kv4_kernel<64, true, false>,   (const void*)decode_kv4_kernel<64, true, true>,
+                         (const void*)decode_kv4_kernel<128, false, false>, (const void*)decode_kv4_kernel<128, false, true>,
+                         (const void*)decode_kv4_kernel<64, false, false>,  (const void*)decode_kv4_kernel<64, false, true>};
     for (const void* f : attend) in_clusters(f);
     for (const void* f : score) in_clusters(f);
+    for (const void* f : kv4) in_clusters(f);
     // the fused decode step wants three CTAs of ~74 KB each on an SM: ask for the largest shared-memory carve-out
     for (const void* f : attend)
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    for (const void* f : kv4)
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     return e;
 }
@@ -839,6 +877,11 @@ cudaError_t ask_decode_room_t(shotkv_ctx* ctx) {
     if (e == cudaSuccess) e = ask_room(decode_attend_kernel<D, true>, AttendCfg<D>::kWarps * 32, attend[1]);
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, false, kDeep>, 256, score[0]);
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, true, kDeep>, 256, score[1]);
+    DecodeRoom(*kv4)[2] = ctx->room_kv4[D == 128];
+    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, false, false>, StepKv4<D, false>::kWarps * 32, kv4[0][0]);
+    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, false, true>, StepKv4<D, false>::kWarps * 32, kv4[0][1]);
+    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, true, false>, StepKv4<D, true>::kWarps * 32, kv4[1][0]);
+    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, true, true>, StepKv4<D, true>::kWarps * 32, kv4[1][1]);
     int* whole = ctx->whole_score[D == 128];
     const auto fit = [&](int& ctas, auto* kernel) {
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, 256, 0);
@@ -1083,6 +1126,113 @@ int shotkv_compact_kv(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_bf1
     return run_compact(ctx, dims, K, V, kept_idx, kept_count, Mcap, Kc, Vc, (cudaStream_t)stream_);
 }
 
+// ---- the kept rows in 4 bits ------------------------------------------------------------------
+namespace {
+int check_kv4(const shotkv_dims* d, int32_t Mcap, const char** why) {
+    if (!d) { *why = "dims is NULL"; return SHOTKV_ERR_INVALID_ARG; }
+    if (d->B < 1 || d->L < 1 || d->Hkv < 1) { *why = "B, L and Hkv must be >= 1"; return SHOTKV_ERR_INVALID_ARG; }
+    if (d->d != 64 && d->d != 128) { *why = "head dimension must be 64 or 128"; return SHOTKV_ERR_UNSUPPORTED_SHAPE; }
+    if (Mcap < 1) { *why = "Mcap must be >= 1"; return SHOTKV_ERR_INVALID_ARG; }
+    if (Mcap > 0x7fffffff - 1024) { *why = "Mcap too large"; return SHOTKV_ERR_UNSUPPORTED_SHAPE; }
+    if ((long long)d->B * d->L > 65535 || d->Hkv > 65535) { *why = "B*L and Hkv must be <= 65535"; return SHOTKV_ERR_UNSUPPORTED_SHAPE; }
+    return SHOTKV_OK;
+}
+}  // namespace
+
+size_t shotkv_kv4_key_bytes(const shotkv_dims* dims, int32_t Mcap) {
+    const char* why = "";
+    return check_kv4(dims, Mcap, &why) ? 0 : (size_t)dims->B * dims->L * dims->Hkv * kv4_unit_bytes(dims, Mcap, false);
+}
+size_t shotkv_kv4_value_bytes(const shotkv_dims* dims, int32_t Mcap) {
+    const char* why = "";
+    return check_kv4(dims, Mcap, &why) ? 0 : (size_t)dims->B * dims->L * dims->Hkv * kv4_unit_bytes(dims, Mcap, true);
+}
+
+int shotkv_compact_kv4(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_bf16* K, const shotkv_bf16* V,
+                       const int32_t* kept_idx, const int32_t* kept_count, int32_t Mcap, void* K4, void* V4, void* stream_) {
+    TraceRange trace_("shotkv_compact_kv4");
+    int rc = set_device(ctx);
+    if (rc) return rc;
+    const char* why = "";
+    if ((rc = check_kv4(dims, Mcap, &why))) return fail(ctx, rc, "%s", why);
+    if (dims->N < 1) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "N must be >= 1");
+    if (!K || !V || !kept_count || !K4 || !V4) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "pointers must not be NULL");
+    if (!aligned16(K, V, K4, V4)) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "K, V, K4 and V4 must be 16-byte aligned");
+    return run_compact_kv4(ctx, dims, K, V, kept_idx, kept_count, Mcap, K4, V4, (cudaStream_t)stream_);
+}
+
+int shotkv_unpack_kv4(shotkv_ctx* ctx, const shotkv_dims* dims, const void* K4, const void* V4, const int32_t* kept_count,
+                      int32_t Mcap, shotkv_bf16* Kc, shotkv_bf16* Vc, void* stream_) {
+    TraceRange trace_("shotkv_unpack_kv4");
+    int rc = set_device(ctx);
+    if (rc) return rc;
+    const char* why = "";
+    if ((rc = check_kv4(dims, Mcap, &why))) return fail(ctx, rc, "%s", why);
+    if (!K4 || !V4 || !kept_count || !Kc || !Vc) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "pointers must not be NULL");
+    if (!aligned16(K4, V4, Kc, Vc)) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "K4, V4, Kc and Vc must be 16-byte aligned");
+    const dim3 grid((2 * kv4_tiles(Mcap) + kPackThreads / 32 - 1) / (kPackThreads / 32), dims->Hkv, dims->B * dims->L);
+    return launch(ctx, dims->d == 128 ? unpack_kv4_kernel<128> : unpack_kv4_kernel<64>, grid, kPackThreads, 0, (cudaStream_t)stream_, 1, kEarly,
+                  (const unsigned char*)K4, (const unsigned char*)V4, kept_count, (int)dims->Hkv, (int)Mcap, (uint4*)Kc, (uint4*)Vc);
+}
+
+// ---- norm, rotation, layout -------------------------------------------------------------------
+namespace {
+int check_rope(const shotkv_dims* d, const shotkv_rope* r, const char** why) {
+    if (!d || !r) { *why = "dims and rope must not be NULL"; return SHOTKV_ERR_INVALID_ARG; }
+    if (d->B < 1 || d->L < 1 || d->H < 1 || d->Hkv < 1 || d->N < 1 || d->W < 1) {
+        *why = "B, L, H, Hkv, N, W must be >= 1"; return SHOTKV_ERR_INVALID_ARG;
+    }
+    if (d->H % d->Hkv != 0) { *why = "H must be a multiple of Hkv"; return SHOTKV_ERR_INVALID_ARG; }
+    if (d->W > d->N) { *why = "window W exceeds N"; return SHOTKV_ERR_INVALID_ARG; }
+    if (d->d != 64 && d->d != 128) { *why = "head dimension must be 64 or 128"; return SHOTKV_ERR_UNSUPPORTED_SHAPE; }
+    if (r->layer < 0 || r->layer >= d->L) { *why = "layer must be in [0, L)"; return SHOTKV_ERR_INVALID_ARG; }
+    if (r->rows < 1 || r->first < 0 || r->first > d->N - r->rows) { *why = "rows first .. first+rows-1 must lie in [0, N)"; return SHOTKV_ERR_INVALID_ARG; }
+    if (r->rot < 0 || r->rot > d->d || r->rot % 16) { *why = "rot must be a multiple of 16 in [0, d]"; return SHOTKV_ERR_INVALID_ARG; }
+    if (r->interleaved != 0 && r->interleaved != 1) { *why = "interleaved must be 0 or 1"; return SHOTKV_ERR_INVALID_ARG; }
+    if (!(r->eps >= 0.f) || !std::isfinite(r->eps)) { *why = "eps must be finite and >= 0"; return SHOTKV_ERR_INVALID_ARG; }
+    if ((r->q_row | r->k_row | r->v_row | r->q_prompt | r->k_prompt | r->v_prompt) & 7) { *why = "strides must be multiples of 8 elements"; return SHOTKV_ERR_INVALID_ARG; }
+    return SHOTKV_OK;
+}
+}  // namespace
+
+int shotkv_norm_rope(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_rope* rope, const shotkv_bf16* q, const shotkv_bf16* k,
+                     const shotkv_bf16* v, const shotkv_bf16* q_weight, const shotkv_bf16* k_weight, const float* cos_sin,
+                     const int32_t* positions, shotkv_bf16* Qwin, shotkv_bf16* K, shotkv_bf16* V, shotkv_bf16* q_out, void* stream_) {
+    TraceRange trace_("shotkv_norm_rope");
+    int rc = set_device(ctx);
+    if (rc) return rc;
+    const char* why = "";
+    if ((rc = check_rope(dims, rope, &why))) return fail(ctx, rc, "%s", why);
+    if (!q || !k || !v || !Qwin || !K || !V) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "pointers must not be NULL");
+    if (rope->rot > 0 && !cos_sin) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "cos_sin must not be NULL when rot > 0");
+    if (rope->rot > 0 && rope->table_rows < 1) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "table_rows must be >= 1");
+    if (!aligned16(q, k, v, q_weight, k_weight, cos_sin, Qwin, K, V, q_out))
+        return fail(ctx, SHOTKV_ERR_INVALID_ARG, "all tensors but positions must be 16-byte aligned");
+    NormRopeParams p{};
+    p.q = (const __nv_bfloat16*)q; p.k = (const __nv_bfloat16*)k; p.v = (const __nv_bfloat16*)v;
+    p.q_row = rope->q_row; p.k_row = rope->k_row; p.v_row = rope->v_row;
+    p.q_prompt = rope->q_prompt; p.k_prompt = rope->k_prompt; p.v_prompt = rope->v_prompt;
+    p.q_weight = (const __nv_bfloat16*)q_weight; p.k_weight = (const __nv_bfloat16*)k_weight;
+    p.table = (const float2*)cos_sin; p.positions = positions;
+    p.Qwin = (__nv_bfloat16*)Qwin; p.K = (__nv_bfloat16*)K; p.V = (__nv_bfloat16*)V; p.q_out = (__nv_bfloat16*)q_out;
+    p.B = dims->B; p.L = dims->L; p.H = dims->H; p.Hkv = dims->Hkv; p.N = dims->N; p.W = dims->W;
+    p.layer = rope->layer; p.first = rope->first; p.rows = rope->rows; p.rot = rope->rot; p.interleaved = rope->interleaved;
+    p.table_rows = rope->table_rows; p.eps = rope->eps;
+    // of the queries all rows, or those in the window
+    const int to_window = dims->N - dims->W - rope->first;
+    p.q_first = q_out || to_window < 0 ? 0 : std::min(to_window, (int)rope->rows);
+    const int section = kRopeAhead * 256 / dims->d;
+    p.kv_sections = (dims->Hkv + section - 1) / section;
+    p.q_sections = (dims->H + section - 1) / section;
+    const long long kv = 2LL * dims->B * rope->rows * p.kv_sections, items = kv + (long long)dims->B * (rope->rows - p.q_first) * p.q_sections;
+    if (items > 0x7fffff00LL) return fail(ctx, SHOTKV_ERR_UNSUPPORTED_SHAPE, "B * rows * heads too large");
+    p.kv_items = (int)kv;
+    p.items = (int)items;
+    constexpr int warps = kRopeThreads / 32;
+    return launch(ctx, dims->d == 128 ? norm_rope_kernel<128> : norm_rope_kernel<64>, dim3((p.items + warps - 1) / warps), kRopeThreads, 0,
+                  (cudaStream_t)stream_, 1, kEarly, p);
+}
+
 namespace {
 // Called on the caller's stream before a group's scoring pass is enqueued (the host-buffer variant
 // copies that group's K there).
@@ -1090,14 +1240,15 @@ using BeforeGroup = std::function<int(const GroupView&, cudaStream_t)>;
 
 int prefill_compress_impl(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_policy* policy, const shotkv_bf16* Qwin,
                           const shotkv_bf16* K, const shotkv_bf16* V, const int32_t* offsets_host, float* shot_scores,
-                          uint8_t* keep, int32_t* kept_idx, int32_t* kept_count, int32_t Mcap, shotkv_bf16* Kc,
-                          shotkv_bf16* Vc, float* token_importance, uint32_t flags, void* ws, size_t ws_bytes,
+                          uint8_t* keep, int32_t* kept_idx, int32_t* kept_count, int32_t Mcap, const KeptRows& to,
+                          float* token_importance, uint32_t flags, void* ws, size_t ws_bytes,
                           void* stream_, const BeforeGroup* before_group) {
     int rc = set_device(ctx);
     if (rc) return rc;
     const char* why = "";
     if ((rc = check_dims(dims, &why))) return fail(ctx, rc, "%s", why);
-    if (!aligned16(Qwin, K, V, Kc, Vc)) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "Qwin, K, V, Kc and Vc must be 16-byte aligned");
+    if (!aligned16(Qwin, K, V, to.K, to.V))
+        return fail(ctx, SHOTKV_ERR_INVALID_ARG, "Qwin, K, V, %s must be 16-byte aligned", to.packed ? "K4 and V4" : "Kc and Vc");
     const bool tokens = (flags & SHOTKV_FLAG_TOKEN_IMPORTANCE) != 0;
     if (tokens || token_route(dims)) {
         // per-token importances first (asked for, or many short units): the three public steps in
@@ -1118,7 +1269,9 @@ int prefill_compress_impl(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv
                                             Mcap, ws, ws_bytes, stream_);
         if (src < 0) return src;
         if (!tokens) prof_mark(ctx, (cudaStream_t)stream_);
-        if ((rc = shotkv_compact_kv(ctx, dims, K, V, kept_idx, kept_count, Mcap, Kc, Vc, stream_)) < 0) return rc;
+        rc = to.packed ? shotkv_compact_kv4(ctx, dims, K, V, kept_idx, kept_count, Mcap, to.K, to.V, stream_)
+                       : shotkv_compact_kv(ctx, dims, K, V, kept_idx, kept_count, Mcap, (shotkv_bf16*)to.K, (shotkv_bf16*)to.V, stream_);
+        if (rc < 0) return rc;
         if (!tokens) prof_mark(ctx, (cudaStream_t)stream_);
         return src;
     }
@@ -1126,7 +1279,7 @@ int prefill_compress_impl(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv
     int worst = 0;
     const int orc = check_offsets(dims, policy, offsets_host, &worst, &why);
     if (orc < 0) return fail(ctx, orc, "%s", why);
-    if (!Qwin || !K || !V || !shot_scores || !keep || !kept_idx || !kept_count || !Kc || !Vc)
+    if (!Qwin || !K || !V || !shot_scores || !keep || !kept_idx || !kept_count || !to.K || !to.V)
         return fail(ctx, SHOTKV_ERR_INVALID_ARG, "pointers must not be NULL");
     const int need = budget_of(dims, policy) > worst ? budget_of(dims, policy) : worst;
     if (Mcap < need) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "Mcap = %d but %d rows may be kept", Mcap, need);
@@ -1178,7 +1331,7 @@ int prefill_compress_impl(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv
                                     select_args(dg, policy, keep + v.bl0 * S1, idx_g, count_g, Mcap), tail))) return bail(rc);
         prof_gmark(ctx, g, 3, tail);                    // reduction and selection are one kernel: the selection's own stage is empty
         prof_gmark(ctx, g, 4, tail);
-        if ((rc = run_compact(ctx, dg, Kg, Vg, idx_g, count_g, Mcap, Kc + v.u0 * (size_t)Mcap * row, Vc + v.u0 * (size_t)Mcap * row, tail))) return bail(rc);
+        if ((rc = run_keep(ctx, dg, Kg, Vg, idx_g, count_g, Mcap, to, v.u0, tail))) return bail(rc);
         prof_gmark(ctx, g, 5, tail);
     }
     if (forked) {
@@ -1196,8 +1349,17 @@ int shotkv_prefill_compress(shotkv_ctx* ctx, const shotkv_dims* dims, const shot
                             shotkv_bf16* Vc, float* token_importance, uint32_t flags, void* ws, size_t ws_bytes,
                             void* stream_) {
     TraceRange trace_("shotkv_prefill_compress");
-    return prefill_compress_impl(ctx, dims, policy, Qwin, K, V, offsets_host, shot_scores, keep, kept_idx, kept_count, Mcap, Kc,
-                                 Vc, token_importance, flags, ws, ws_bytes, stream_, nullptr);
+    return prefill_compress_impl(ctx, dims, policy, Qwin, K, V, offsets_host, shot_scores, keep, kept_idx, kept_count, Mcap,
+                                 KeptRows{Kc, Vc, false}, token_importance, flags, ws, ws_bytes, stream_, nullptr);
+}
+
+int shotkv_prefill_compress_kv4(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_policy* policy, const shotkv_bf16* Qwin,
+                                const shotkv_bf16* K, const shotkv_bf16* V, const int32_t* offsets_host, float* shot_scores,
+                                uint8_t* keep, int32_t* kept_idx, int32_t* kept_count, int32_t Mcap, void* K4, void* V4,
+                                float* token_importance, uint32_t flags, void* ws, size_t ws_bytes, void* stream_) {
+    TraceRange trace_("shotkv_prefill_compress_kv4");
+    return prefill_compress_impl(ctx, dims, policy, Qwin, K, V, offsets_host, shot_scores, keep, kept_idx, kept_count, Mcap,
+                                 KeptRows{K4, V4, true}, token_importance, flags, ws, ws_bytes, stream_, nullptr);
 }
 
 // ---- host-buffer variant -------------------------------------------------------------------
@@ -1285,7 +1447,7 @@ int shotkv_prefill_compress_host(shotkv_ctx* ctx, const shotkv_dims* dims, const
         V_in = a.V;
     }
     const int prc = prefill_compress_impl(ctx, dims, policy, a.Q, a.K, V_in, offsets_host, a.scores, a.keep, a.idx, a.count,
-                                          Mcap, Kc_out ? Kc_out : a.Kc, Vc_out ? Vc_out : a.Vc, nullptr, 0, a.ws,
+                                          Mcap, KeptRows{Kc_out ? Kc_out : a.Kc, Vc_out ? Vc_out : a.Vc, false}, nullptr, 0, a.ws,
                                           a.ws_bytes, stream_, &copy_k);
     if (prc < 0) return prc;
     const size_t S1 = dims->S > 0 ? dims->S : 1;
@@ -1364,7 +1526,7 @@ namespace {
 // 2, 185 keys 8.5 -> 7.1; 1 block: 8 heads of 1,150 keys 7.0 -> 7.3).  Scores alone take less per block than a larger
 // cluster costs (8 heads of 3,400 keys 5.3 us with 2.5 blocks, 6.1 with 2, 5.7 with 3; with 2.5, 1 to 148 units of 64
 // to 8,192 keys all take what they took with 2 and at most eight CTAs, within 2 %, or less).
-constexpr int kLeastAttend = 8, kLeastScore = 15;
+constexpr int kLeastAttend = 8, kLeastScore = 15, kLeastKv4 = 12;
 template <class Smem>
 int decode_split(const DecodeRoom& room, Smem&& smem, long long U, long long keys, int warps, int least) {
     int n = kMaxSplit;
@@ -1447,17 +1609,42 @@ int launch_decode_score(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishPara
     return launch(ctx, kernel, grid, 256, whole, stream, 1, kEarly, p, f);
 }
 
-// One decode step; with `attn_out` the score kernel is the variant that also writes the attention output.
+// The same over a prompt in 4 bits.
+template <int D, bool ATTEND>
+int launch_decode_kv4_t(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
+                        cudaStream_t stream) {
+    constexpr int threads = StepKv4<D, ATTEND>::kWarps * 32;
+    const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND];
+    const auto smem_of = [&](int n) { return kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, n); };
+    p.nsplit = decode_split(room[0], smem_of, U, (long long)p.Mcap + p.n_old + 1, StepKv4<D, ATTEND>::kWarps, kLeastKv4);
+    const size_t smem = smem_of(p.nsplit), end = fused_end_smem_bytes(p.Hkv, f.n, f.k < f.n);
+    const dim3 grid(U * p.nsplit);
+    ended = smem + end <= kBigSmem &&
+            ends_fused(ctx, room[1].with(smem + end), p, f, U, threads, ATTEND ? kFusedEntriesAttend : kFusedEntriesScore);
+    if (ended) return launch(ctx, decode_kv4_kernel<D, ATTEND, true>, grid, threads, smem + end, stream, p.Hkv * p.nsplit, kEarly, p, f, cache);
+    if (smem > kBigSmem) return fail(ctx, SHOTKV_ERR_UNSUPPORTED_SHAPE, "Dcap too large for the step over a packed cache");
+    return launch(ctx, decode_kv4_kernel<D, ATTEND, false>, grid, threads, smem, stream, p.nsplit, kEarly, p, f, cache);
+}
+int launch_decode_kv4(shotkv_ctx* ctx, int d, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
+                      cudaStream_t stream) {
+    const auto run = p.out ? (d == 128 ? launch_decode_kv4_t<128, true> : launch_decode_kv4_t<64, true>)
+                           : (d == 128 ? launch_decode_kv4_t<128, false> : launch_decode_kv4_t<64, false>);
+    return run(ctx, p, f, cache, U, ended, stream);
+}
+
+// One decode step; with `attn_out` the score kernel is the variant that also writes the attention output.  `packed`: Kc and Vc
+// are K4 and V4.
 int decode_step_impl(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16* q, const shotkv_bf16* k_new,
-                     const shotkv_bf16* v_new, const shotkv_bf16* Kc, const shotkv_bf16* Vc, const int32_t* kept_count,
-                     float* attn_out, void* stream_) {
+                     const shotkv_bf16* v_new, const void* Kc, const void* Vc, const int32_t* kept_count,
+                     float* attn_out, bool packed, void* stream_) {
     int rc = set_device(ctx);
     if (rc) return rc;
     if (!st || !q || !k_new || !v_new || !kept_count) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "pointers must not be NULL");
-    if (st->Mcap > 0 && !Kc) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "Kc must not be NULL when Mcap > 0");
-    if (attn_out && st->Mcap > 0 && !Vc) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "Vc must not be NULL when Mcap > 0");
+    if (st->Mcap > 0 && !Kc) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "%s must not be NULL when Mcap > 0", packed ? "K4" : "Kc");
+    if (attn_out && st->Mcap > 0 && !Vc) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "%s must not be NULL when Mcap > 0", packed ? "V4" : "Vc");
     if (!aligned16(q, k_new, v_new)) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "q, k_new and v_new must be 16-byte aligned");
-    if (st->Mcap > 0 && !aligned16(Kc, attn_out ? Vc : nullptr)) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "Kc and Vc must be 16-byte aligned");
+    if (st->Mcap > 0 && !aligned16(Kc, attn_out ? Vc : nullptr))
+        return fail(ctx, SHOTKV_ERR_INVALID_ARG, "%s must be 16-byte aligned", packed ? "K4 and V4" : "Kc and Vc");
     if (st->n_dec + 1 > st->Dcap) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "decode region full: n_dec = %d, Dcap = %d", st->n_dec, st->Dcap);
     cudaStream_t stream = (cudaStream_t)stream_;
     const shotkv_dims& d = st->dims;
@@ -1489,12 +1676,17 @@ int decode_step_impl(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16
     bool ended = false;                                   // the step ends in this kernel
     prof_begin(ctx);
     prof_mark(ctx, stream);
-    const auto first = attn_out ? (d.d == 128 ? launch_decode_attend<128> : launch_decode_attend<64>)
-                                : (d.d == 128 ? launch_decode_score<128> : launch_decode_score<64>);
-    if ((rc = first(ctx, p, f, U, ended, stream))) return rc;
+    if (packed) {
+        rc = launch_decode_kv4(ctx, d.d, p, f, PackedCache{(const unsigned char*)Kc, (const unsigned char*)Vc}, U, ended, stream);
+    } else {
+        const auto first = attn_out ? (d.d == 128 ? launch_decode_attend<128> : launch_decode_attend<64>)
+                                    : (d.d == 128 ? launch_decode_score<128> : launch_decode_score<64>);
+        rc = first(ctx, p, f, U, ended, stream);
+    }
+    if (rc) return rc;
     prof_mark(ctx, stream);
 
-    const int how = kEarly | (attn_out && two_to_an_sm(ctx, p, U, d.d) ? kWideShared : 0);
+    const int how = kEarly | (attn_out && !packed && two_to_an_sm(ctx, p, U, d.d) ? kWideShared : 0);
     if (!ended && f.k < f.n) {
         f.ranks = d.Hkv < kReduceCluster ? d.Hkv : kReduceCluster;
         rc = launch(ctx, d.d == 128 ? decode_evict_kernel<128> : decode_evict_kernel<64>, dim3(BL * f.ranks), kSelectThreads,
@@ -1517,7 +1709,7 @@ extern "C" {
 int shotkv_decode_step(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16* q, const shotkv_bf16* k_new,
                        const shotkv_bf16* v_new, const shotkv_bf16* Kc, const int32_t* kept_count, void* stream) {
     TraceRange trace_("shotkv_decode_step");
-    return decode_step_impl(ctx, st, q, k_new, v_new, Kc, nullptr, kept_count, nullptr, stream);
+    return decode_step_impl(ctx, st, q, k_new, v_new, Kc, nullptr, kept_count, nullptr, false, stream);
 }
 
 int shotkv_decode_step_attend(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16* q, const shotkv_bf16* k_new,
@@ -1525,7 +1717,21 @@ int shotkv_decode_step_attend(shotkv_ctx* ctx, shotkv_decode_state* st, const sh
                               const int32_t* kept_count, float* attn_out, void* stream) {
     TraceRange trace_("shotkv_decode_step_attend");
     if (!attn_out) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "attn_out must not be NULL");
-    return decode_step_impl(ctx, st, q, k_new, v_new, Kc, Vc, kept_count, attn_out, stream);
+    return decode_step_impl(ctx, st, q, k_new, v_new, Kc, Vc, kept_count, attn_out, false, stream);
+}
+
+int shotkv_decode_step_kv4(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16* q, const shotkv_bf16* k_new,
+                           const shotkv_bf16* v_new, const void* K4, const int32_t* kept_count, void* stream) {
+    TraceRange trace_("shotkv_decode_step_kv4");
+    return decode_step_impl(ctx, st, q, k_new, v_new, K4, nullptr, kept_count, nullptr, true, stream);
+}
+
+int shotkv_decode_step_attend_kv4(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16* q, const shotkv_bf16* k_new,
+                                  const shotkv_bf16* v_new, const void* K4, const void* V4, const int32_t* kept_count,
+                                  float* attn_out, void* stream) {
+    TraceRange trace_("shotkv_decode_step_attend_kv4");
+    if (!attn_out) return fail(ctx, SHOTKV_ERR_INVALID_ARG, "attn_out must not be NULL");
+    return decode_step_impl(ctx, st, q, k_new, v_new, K4, V4, kept_count, attn_out, true, stream);
 }
 
 int32_t shotkv_plan_pieces(const shotkv_dims* dims, const int32_t* offsets_host, int32_t sm_count, int32_t* nchunk,
