@@ -136,17 +136,18 @@ __device__ __forceinline__ void send(float4* to, int rank, unsigned long long* b
 }
 // Waits, `limit` cycles at most, until all bytes expected are there.  False: it gave up and has set the error word; what it
 // waited for may still come, so the thread passes outlive_messages before it ends.
-__device__ __forceinline__ bool await_messages(unsigned long long* bar, int* err, long long limit) {
+// `parity`: of the barrier's phase that is waited for (one that is used once is in phase 0).
+__device__ __forceinline__ bool await_messages(unsigned long long* bar, int* err, long long limit, uint32_t parity = 0) {
     const uint32_t b = smem_u32(bar);
     const long long t0 = clock64();
     for (;;) {
         uint32_t done;
         asm volatile(
             "{\n\t.reg .pred q;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 q, [%1], 0;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 q, [%1], %2;\n\t"
             "selp.u32 %0, 1, 0, q;\n\t}"
             : "=r"(done)
-            : "r"(b)
+            : "r"(b), "r"(parity)
             : "memory");
         if (done) return true;
         if (clock64() - t0 > limit) {

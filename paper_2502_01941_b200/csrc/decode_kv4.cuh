@@ -4,6 +4,7 @@
 
 #include "decode.cuh"
 #include "kv4.cuh"
+#include "score_tc.cuh"
 
 namespace shotkv {
 
@@ -13,6 +14,13 @@ __device__ __forceinline__ void mma_f16_16816(float (&c)[4], const uint32_t (&a)
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same with nothing to add to.  (With zeros in the accumulator beforehand they were 60 moves a tile.)
+__device__ __forceinline__ void mma_f16_16816_first(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 // An 8x8 matrix of 16-bit elements, two neighbours of row lane / 4 a lane, transposed.
 __device__ __forceinline__ uint32_t transposed(uint32_t a) {
@@ -26,6 +34,13 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 }
 __device__ __forceinline__ float2 unpack_f16(uint32_t a) { return __half22float2(*reinterpret_cast<const __half2*>(&a)); }
 
+// `bytes` (a multiple of 16) from global to this CTA's shared memory; they are counted on the barrier when they have landed.
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes),
+                 "r"(bar)
+                 : "memory");
+}
+
 struct PackedCache {
     const unsigned char *K4, *V4;            // [U][tiles][Kv4 tile]
 };
@@ -36,12 +51,15 @@ struct StepKv4 {
     static constexpr int kStages = ATTEND ? 2 : 3;         // tiles in a warp's ring
     static constexpr int kStageBytes = Kv4<D>::kKeyTile + (ATTEND ? Kv4<D>::kValueTile : 0);
     static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
+    static constexpr int kBarBytes = kWarps * kStages * 8;
+    static constexpr int kQueryBytes = 8 * D * 2 + (D / 32) * 8 * 4;    // fragments of 8 rows in f16, their groups' sums
     static_assert(!ATTEND || 8 * kOutPitch<D> * 4 <= kStages * kStageBytes, "a warp's outputs take the place of its ring");
 };
 template <int D, bool ATTEND>
 __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit) {
     const size_t shares = nsplit > 1 ? (size_t)nsplit * (16 + (ATTEND ? (G * D / 4 / nsplit + 1) * 4 : 0)) : 0;
-    return StepKv4<D, ATTEND>::kRingBytes + 16 + ((size_t)StepKv4<D, ATTEND>::kWarps * 16 + ((size_t)G * Dcap + 3) / 4 * 4 + shares) * 4;
+    using Cfg = StepKv4<D, ATTEND>;
+    return Cfg::kRingBytes + Cfg::kBarBytes + Cfg::kQueryBytes + 16 + ((size_t)Cfg::kWarps * 16 + ((size_t)G * Dcap + 3) / 4 * 4 + shares) * 4;
 }
 
 // decode_score_kernel's and (ATTEND) decode_attend_kernel's step over packed prefill rows.  A warp takes decode entries,
@@ -54,14 +72,18 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 //     down to 2^-31 of it exact.  A logit is sum over groups s (S + z sum of q's 32 elements).
 //   O^T[16 dims x 8 rows] += codes^T . w^T with w = p s_v, p = 2^(logit - reference): the accumulator of S, transposed 8 by 8, is
 //     the other operand, an f16 pair (high part and remainder: 2^-22 of w, or 2^-35 of the row's largest where that is more).  z
-//     is added once a row: sum of w z_v.
+//     is added once a row: sum of w z_v.  PAIRED, for groups of up to four rows: the remainders are columns 4 .. 7 of the one
+//     operand whose columns 0 .. 3 are the high parts, so that one product does for both.  (8 sequences x 32 layers, four rows:
+//     MMM us a step, MMM with a product for each part.)
 //
 // f16 ends at 65504, so both factors are kept in range by references that change seldom: a row's reference is 2^10 below its
 // maximum when it was last set and is set again by a tile whose p would exceed 2^13, and the values' scales are multiplied by a
-// power of two that takes the largest of the first tile to [1, 2) and is set again when one exceeds 4.  One vote a
-// half tile decides that neither has happened.
-template <int D, bool ATTEND, bool FUSED>
-__global__ void __launch_bounds__(StepKv4<D, ATTEND>::kWarps * 32, 4)
+// power of two that takes the largest of the first tile to [1, 2) and is set again when one exceeds 4.  One vote a tile
+// decides that neither has happened.  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
+// products are summed for themselves and then added (one sum for all of a warp's 26 tiles: outputs 4.2e-6 off in the
+// 2-norm, so 0.00e-7).
+template <int D, bool ATTEND, bool FUSED, bool PAIRED>
+__global__ void __launch_bounds__(StepKv4<D, ATTEND>::kWarps * 32, FUSED ? 3 : ATTEND ? 4 : 5)
 decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const PackedCache cache) {
     using Cfg = StepKv4<D, ATTEND>;
     using F = Kv4<D>;
@@ -70,7 +92,9 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     constexpr float kLift = 10.f, kHighest = 13.f, kUnset = -1e30f;
     extern __shared__ __align__(128) unsigned char dsm[];
     unsigned char* ring = dsm;                               // [NW][NS][keys | values]; later each warp's outputs
-    float2* sred = reinterpret_cast<float2*>(ring + Cfg::kRingBytes + 16);   // [NW warps][8 rows]  (m, z)
+    uint4* sq = reinterpret_cast<uint4*>(ring + Cfg::kRingBytes + Cfg::kBarBytes);   // [NB][32 lanes] the queries as B fragments, f16
+    float* sqsum = reinterpret_cast<float*>(sq + NB * 32);                   // [NB][8 rows] their groups' sums
+    float2* sred = reinterpret_cast<float2*>(ring + Cfg::kRingBytes + Cfg::kBarBytes + Cfg::kQueryBytes + 16);   // [NW warps][8 rows]  (m, z)
     float* sdec = reinterpret_cast<float*>(sred + NW * 8);   // [G][Dcap]  logits of the decode entries
     float2* stab = reinterpret_cast<float2*>(sdec + ((p.G * p.Dcap + 3) & ~3));
     float4* sin = reinterpret_cast<float4*>(stab + p.nsplit * 8);
@@ -84,6 +108,13 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     const int first_cta = FUSED ? hk * p.nsplit : 0, ctas = p.Hkv * p.nsplit;   // in the cluster: the unit's first; FUSED: all
     FusedEnd end{};
     if (FUSED) end = fused_end_at(dsm + kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, p.nsplit), f);
+    unsigned long long* bars = reinterpret_cast<unsigned long long*>(ring + Cfg::kRingBytes) + warp * NS;   // this warp's stages'
+    if (lane == 0) {
+#pragma unroll
+        for (int k = 0; k < NS; ++k) tc::mbar_init(smem_u32(bars + k), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    __syncwarp();
     if (FUSED || p.nsplit > 1) {
         if (tid == 0) {
             if (p.nsplit > 1) expect_messages(arrived, p.nsplit * (8 * (int)sizeof(float2) + (ATTEND ? qs.owned * (int)sizeof(float4) : 0)));
@@ -98,13 +129,14 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     const uint4* knew_u = reinterpret_cast<const uint4*>(p.k_new + (size_t)u * D);
     const uint4* vnew_u = reinterpret_cast<const uint4*>(p.v_new + (size_t)u * D);
     const int kept = p.kept_count[bl];
-    // query row g of the group as B fragments, bf16
+    // query rows as B fragments: columns 0 .. 7 are the group's rows, or (PAIRED) its up to four rows twice.  This lane's column of
+    // an operand is g, and of an accumulator 2*t4 and 2*t4 + 1, which are rows r0 and r0 + 1.
+    const int g_row = PAIRED ? g & 3 : g, r0 = PAIRED ? (2 * t4) & 3 : 2 * t4;
+    const bool second = PAIRED && t4 >= 2;                   // the columns of the weights' remainders
+    const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bl * p.H + (size_t)hk * p.G + g_row) * D);
     uint4 qf[NB];
-    {
-        const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bl * p.H + (size_t)hk * p.G + g) * D);
 #pragma unroll
-        for (int kb = 0; kb < NB; ++kb) qf[kb] = g < p.G ? qrow[kb * 4 + t4] : make_uint4(0, 0, 0, 0);
-    }
+    for (int kb = 0; kb < NB; ++kb) qf[kb] = load_if(qrow + kb * 4 + t4, g_row < p.G);
     const bool appends = rank == 0 && tid < 2 * VPR;         // the CTA that appends the new token's rows
     uint4 fresh_row = make_uint4(0, 0, 0, 0);
     if (appends) fresh_row = (tid < VPR ? knew_u + tid : vnew_u + (tid - VPR))[0];
@@ -116,28 +148,62 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     const int all_tiles = kv4_tiles(p.Mcap);
     const unsigned char* Kt_u = cache.K4 + (size_t)u * all_tiles * F::kKeyTile;
     const unsigned char* Vt_u = cache.V4 + (size_t)u * all_tiles * F::kValueTile;
-    const uint32_t wring = smem_u32(ring) + (uint32_t)(warp * NS * Cfg::kStageBytes);
-    const auto copy = [&](uint32_t to, const unsigned char* from, auto bytes) {
-        constexpr int N = decltype(bytes)::value / 16;       // 16-byte pieces
-#pragma unroll
-        for (int k = 0; k < (N + 31) / 32; ++k)
-            if (k * 32 + 32 <= N || lane < N - k * 32) cp_async16(to + (uint32_t)(k * 512 + lane * 16), from + k * 512 + lane * 16);
-    };
+    const unsigned char* mine = ring + warp * NS * Cfg::kStageBytes;         // this warp's ring
+    // One lane asks for a tile, in one copy of its keys and one of its values: as 16-byte copies, ten a lane, these and
+    // their addresses were a tenth of the loop's instructions.
     const auto fetch = [&](int tile, int stage) {
-        const uint32_t st = wring + (uint32_t)(stage * Cfg::kStageBytes);
-        copy(st, Kt_u + (size_t)tile * F::kKeyTile, std::integral_constant<int, F::kKeyTile>());
-        if (ATTEND) copy(st + F::kKeyTile, Vt_u + (size_t)tile * F::kValueTile, std::integral_constant<int, F::kValueTile>());
-        cp_async_commit();
+        if (lane != 0) return;
+        const uint32_t st = smem_u32(mine) + (uint32_t)(stage * Cfg::kStageBytes), bar = smem_u32(bars + stage);
+        tc::mbar_expect_tx(bar, Cfg::kStageBytes);
+        bulk_load(st, Kt_u + (size_t)tile * F::kKeyTile, F::kKeyTile, bar);
+        if (ATTEND) bulk_load(st + F::kKeyTile, Vt_u + (size_t)tile * F::kValueTile, F::kValueTile, bar);
     };
-    // the first tiles are asked for before the kept count is there: tiles below the cap can be read
+    // The first are asked for before the kept count is there: tiles below the cap can be read.
 #pragma unroll
-    for (int k = 0; k < NS; ++k) {
+    for (int k = 0; k < NS; ++k)
         if (first_tile + k * step < all_tiles) fetch(first_tile + k * step, k);
-        else cp_async_commit();
-    }
     if (FUSED || p.nsplit > 1) cluster_wait();               // all CTAs of the cluster have begun: their memory may be written to
     if (appends)                                             // decode entry n_old
         (tid < VPR ? Kd_u + (size_t)p.n_old * VPR + tid : Vd_u + (size_t)p.n_old * VPR + (tid - VPR))[0] = fresh_row;
+
+    // The queries in f16, the sums of their groups, and what a logit is multiplied by.  They lie in shared memory: in
+    // registers they would take a CTA from the SM.
+    float scale2[2];                                         // of rows 2*t4 and 2*t4 + 1
+    {
+        float top = 0.f;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const uint32_t e[4] = {qf[kb].x, qf[kb].y, qf[kb].z, qf[kb].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf16_low(e[i])), fabsf(bf16_high(e[i]))));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const int power = min(max((int)(__float_as_uint(top) >> 23), 27), 254) - 141;          // top is about 2^(power + 14)
+        const float down = __uint_as_float((uint32_t)(127 - power) << 23);                     // 2^-power
+        const float scale = p.scale_log2 * 0x1p24f * __uint_as_float((uint32_t)(127 + power) << 23);
+#pragma unroll
+        for (int r = 0; r < 2; ++r) scale2[r] = __shfl_sync(0xffffffffu, scale, 8 * t4 + 4 * r);
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            uint32_t e[4] = {qf[kb].x, qf[kb].y, qf[kb].z, qf[kb].w};
+            float s = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                e[i] = pack_f16(bf16_low(e[i]) * down, bf16_high(e[i]) * down);
+                const float2 v = unpack_f16(e[i]);
+                s += v.x + v.y;
+            }
+            s += __shfl_xor_sync(0xffffffffu, s, 1);
+            s += __shfl_xor_sync(0xffffffffu, s, 2);
+            if (warp == kb) {
+                sq[kb * 32 + lane] = make_uint4(e[0], e[1], e[2], e[3]);
+                if (t4 == 0) sqsum[kb * 8 + g] = s * 0x1p-24f;
+            }
+        }
+    }
+    static_assert(NB <= NW, "a warp writes one block of the queries");
+    __syncthreads();
 
     float O[ATTEND ? MT : 1][4];
 #pragma unroll
@@ -146,11 +212,10 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         for (int c = 0; c < 4; ++c) O[mt][c] = 0.f;
     // of query rows 2*t4 and 2*t4 + 1: the reference (the same in the 8 lanes of a t4), this lane's part of the sum of p, and of w z_v
     float ref[2] = {kUnset, kUnset}, z[2] = {0.f, 0.f}, wz[2] = {0.f, 0.f};
-    // lane's logits x[0..1] of key g, x[2..3] of key g + 8, each of rows 2*t4, 2*t4 + 1
-    const auto raise = [&](const float (&x)[4]) {            // new references, for all lanes
+    const auto raise = [&](const float (&high)[2]) {         // new references, from all lanes' greatest logits
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            float m = fmaxf(x[r], x[2 + r]);
+            float m = high[r];
 #pragma unroll
             for (int o = 4; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             const float up = fmaxf(ref[r], m - kLift);
@@ -182,40 +247,42 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             for (int kb = 0; kb < NB; ++kb) {
                 const uint32_t f0[4] = {a[kb].x, b[kb].x, a[kb].y, b[kb].y};
                 const uint32_t f1[4] = {a[kb].z, b[kb].z, a[kb].w, b[kb].w};
-                mma_bf16_16816(c, f0, qf[kb].x, qf[kb].y);
-                mma_bf16_16816(c, f1, qf[kb].z, qf[kb].w);
+                const uint4 q = load_if(qrow + kb * 4 + t4, g_row < p.G);
+                mma_bf16_16816(c, f0, q.x, q.y);
+                mma_bf16_16816(c, f1, q.z, q.w);
             }
         }
         float x[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int j = base + g + 8 * (i >> 1), r = 2 * t4 + (i & 1);
+            const int j = base + g + 8 * (i >> 1), r = r0 + (i & 1);
             x[i] = j < n ? c[i] * p.scale_log2 : SHOTKV_NEG_INF;
-            if (j < n && r < p.G) sdec[r * p.Dcap + j] = x[i];
+            if (j < n && r < p.G && !second) sdec[r * p.Dcap + j] = x[i];
         }
-        float y[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = x[i] - ref[i & 1];
-        if (__any_sync(0xffffffffu, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) > kHighest)) {
-            raise(x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = x[i] - ref[i & 1];
-        }
+        const float high[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+        if (__any_sync(0xffffffffu, high[0] > ref[0] + kHighest || high[1] > ref[1] + kHighest)) raise(high);
         float w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            w[i] = ex2f(y[i]);
+            w[i] = ex2f(x[i] - ref[i & 1]);
             z[i & 1] += w[i];
         }
         if (ATTEND) {
-            // weights as B fragments in three bf16 parts (2^-24), keys in their order on the product's inner side
+            // weights as B fragments in three bf16 parts (2^-24), keys in their order on the product's inner side; paired, the
+            // first two are one fragment
+            constexpr int PARTS = PAIRED ? 2 : 3;
             uint32_t b0[3], b1[3];
 #pragma unroll
             for (int s = 0; s < 3; ++s) {
-                const uint32_t lo = pack_bf16(w[0], w[1]), hi = pack_bf16(w[2], w[3]);
-                w[0] -= bf16_low(lo), w[1] -= bf16_high(lo), w[2] -= bf16_low(hi), w[3] -= bf16_high(hi);
-                b0[s] = transposed(lo), b1[s] = transposed(hi);
+                b0[s] = pack_bf16(w[0], w[1]), b1[s] = pack_bf16(w[2], w[3]);
+                w[0] -= bf16_low(b0[s]), w[1] -= bf16_high(b0[s]), w[2] -= bf16_low(b1[s]), w[3] -= bf16_high(b1[s]);
             }
+            if (PAIRED) {
+                b0[0] = second ? b0[1] : b0[0], b1[0] = second ? b1[1] : b1[0];
+                b0[1] = second ? 0u : b0[2], b1[1] = second ? 0u : b1[2];
+            }
+#pragma unroll
+            for (int s = 0; s < PARTS; ++s) b0[s] = transposed(b0[s]), b1[s] = transposed(b1[s]);
             // 16 bytes (8 dimensions) a lane of rows 2*t4, 2*t4 + 1, 2*t4 + 8, 2*t4 + 9: the pairs of a fragment lie in two of them
 #pragma unroll
             for (int h = 0; h < NC; ++h) {
@@ -232,65 +299,40 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     const uint32_t a[4] = {__byte_perm(e[0][i], e[1][i], 0x5410), __byte_perm(e[0][i], e[1][i], 0x7632),
                                            __byte_perm(e[2][i], e[3][i], 0x5410), __byte_perm(e[2][i], e[3][i], 0x7632)};
 #pragma unroll
-                    for (int s = 0; s < 3; ++s) mma_bf16_16816(O[h * 4 + i], a, b0[s], b1[s]);
+                    for (int s = 0; s < PARTS; ++s) mma_bf16_16816(O[h * 4 + i], a, b0[s], b1[s]);
                 }
             }
         }
     }
 
     // ---- packed rows
-    // the queries in f16, the sums of their groups, and what a logit is multiplied by
-    float top = 0.f;
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) {
-        const uint32_t e[4] = {qf[kb].x, qf[kb].y, qf[kb].z, qf[kb].w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(bf16_low(e[i])), fabsf(bf16_high(e[i]))));
-    }
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const int power = min(max((int)(__float_as_uint(top) >> 23), 27), 254) - 141;          // top is about 2^(power + 14)
-    const float down = __uint_as_float((uint32_t)(127 - power) << 23);                     // 2^-power
-    float qsum[NB];
-#pragma unroll
-    for (int kb = 0; kb < NB; ++kb) {
-        uint32_t e[4] = {qf[kb].x, qf[kb].y, qf[kb].z, qf[kb].w};
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            e[i] = pack_f16(bf16_low(e[i]) * down, bf16_high(e[i]) * down);
-            const float2 v = unpack_f16(e[i]);
-            s += v.x + v.y;
-        }
-        qf[kb] = make_uint4(e[0], e[1], e[2], e[3]);
-        s += __shfl_xor_sync(0xffffffffu, s, 1);
-        qsum[kb] = s + __shfl_xor_sync(0xffffffffu, s, 2);
-    }
-    const float scale = p.scale_log2 * __uint_as_float((uint32_t)(127 + power) << 23);
-    float qs2[NB][2], scale2[2];                             // of rows 2*t4 and 2*t4 + 1
-#pragma unroll
-    for (int r = 0; r < 2; ++r) {
-        scale2[r] = __shfl_sync(0xffffffffu, scale, 8 * t4 + 4 * r);
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb) qs2[kb][r] = __shfl_sync(0xffffffffu, qsum[kb], 8 * t4 + 4 * r);
-    }
-
     const int M = min(kept, p.Mcap), tiles = kv4_tiles(M);
+    const uint64_t scales = tc::pack2(scale2[0], scale2[1]), scales16 = tc::pack2(scale2[0] * 0.0625f, scale2[1] * 0.0625f);
     float unit = 1.f;                                        // O and wz are in units of 1 / unit
     bool begun = false;
     int stage = 0;
-#pragma unroll 1
-    for (int tile = first_tile; tile < tiles; tile += step) {
-        cp_async_wait<NS - 1>();
+    uint32_t parity = 0;
+    long long limit = p.wait_cycles;                         // 0 once a wait gave up: what is there is computed with, nothing is asked for
+    const auto landed = [&] {
+        if (!tc::mbar_try(smem_u32(bars + stage), parity) && !await_messages(bars + stage, p.err, limit, parity)) limit = 0;
         __syncwarp();
-        const unsigned char* st = ring + (size_t)(warp * NS + stage) * Cfg::kStageBytes;
+    };
+    const auto advance = [&] {
+        stage = stage + 1 == NS ? 0 : stage + 1;
+        if (stage == 0) parity ^= 1;
+    };
+    int tile = first_tile;
+#pragma unroll 1
+    for (; tile < tiles; tile += step) {
+        landed();
+        const unsigned char* st = mine + stage * Cfg::kStageBytes;
+        // of the tile's halves hb: keys 16 hb + g (x[hb][0..1]: rows 2*t4, 2*t4 + 1) and 16 hb + g + 8 (x[hb][2..3])
+        float x[2][4] = {};
+        uint32_t va[2], vb[2];                               // the values' words of these rows
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-            const int key0 = tile * 32 + hb * 16;
-            if (hb == 1 && key0 >= M) break;
             const uint4* kc = reinterpret_cast<const uint4*>(st + hb * F::kHalfBytes) + lane;
             const uint32_t* km = reinterpret_cast<const uint32_t*>(st + F::kCodeBytes) + (hb * 16 + g) * NB;
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
             uint32_t ma[NB], mb[NB];
             if constexpr (NB == 4) {
                 const uint4 a = *reinterpret_cast<const uint4*>(km), b = *reinterpret_cast<const uint4*>(km + 8 * NB);
@@ -299,50 +341,56 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                 const uint2 a = *reinterpret_cast<const uint2*>(km), b = *reinterpret_cast<const uint2*>(km + 8 * NB);
                 ma[0] = a.x, ma[1] = a.y, mb[0] = b.x, mb[1] = b.y;
             }
+            if (ATTEND) {
+                const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + F::kKeyTile + F::kCodeBytes) + hb * 16 + g;
+                va[hb] = vm[0], vb[hb] = vm[8];
+            }
 #pragma unroll
             for (int h = 0; h < NC; ++h) {
                 const uint4 kw = kc[h * 32];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const int kb = 2 * h + i;
-                    float c[4] = {0.f, 0.f, 0.f, 0.f};
+                    const uint4 q = sq[kb * 32 + lane];
+                    const float2 qsum = *reinterpret_cast<const float2*>(sqsum + kb * 8 + r0);
+                    float c[4];
                     uint32_t a[4];
-                    codes_f16(i ? kw.z : kw.x, a);
-                    mma_f16_16816(c, a, qf[kb].x, qf[kb].y);
-                    codes_f16(i ? kw.w : kw.y, a);
-                    mma_f16_16816(c, a, qf[kb].z, qf[kb].w);
-                    const float sa = bf16_high(ma[kb]), za = bf16_low(ma[kb]), sb = bf16_high(mb[kb]), zb = bf16_low(mb[kb]);
-                    x[0] = fmaf(sa, fmaf(za, qs2[kb][0], c[0]), x[0]);
-                    x[1] = fmaf(sa, fmaf(za, qs2[kb][1], c[1]), x[1]);
-                    x[2] = fmaf(sb, fmaf(zb, qs2[kb][0], c[2]), x[2]);
-                    x[3] = fmaf(sb, fmaf(zb, qs2[kb][1], c[3]), x[3]);
+                    codes_subnormal(i ? kw.z : kw.x, a);
+                    mma_f16_16816_first(c, a, q.x, q.y);
+                    codes_subnormal(i ? kw.w : kw.y, a);
+                    mma_f16_16816(c, a, q.z, q.w);
+                    // c + 8 was multiplied, and of key g + 8 sixteen times that, as which its logits remain for now
+                    const float sa = bf16_high(ma[kb]), za = bf16_low(ma[kb]) - 8.f;
+                    const float sb = bf16_high(mb[kb]), zb = fmaf(bf16_low(mb[kb]), 16.f, -128.f);
+                    x[hb][0] = fmaf(sa, fmaf(za, qsum.x, c[0]), x[hb][0]);
+                    x[hb][1] = fmaf(sa, fmaf(za, qsum.y, c[1]), x[hb][1]);
+                    x[hb][2] = fmaf(sb, fmaf(zb, qsum.x, c[2]), x[hb][2]);
+                    x[hb][3] = fmaf(sb, fmaf(zb, qsum.y, c[3]), x[hb][3]);
                 }
             }
+        }
+        if (tile * 32 + 32 > M)                              // rows past the count
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] *= scale2[i & 1];
-            uint32_t va = 0, vb = 0;                         // the values' words of rows g and g + 8
+            for (int hb = 0; hb < 2; ++hb) {
+                const int key = tile * 32 + hb * 16 + g;
+                if (key >= M) x[hb][0] = x[hb][1] = SHOTKV_NEG_INF, va[hb] = 0;
+                if (key + 8 >= M) x[hb][2] = x[hb][3] = SHOTKV_NEG_INF, vb[hb] = 0;
+            }
+        bool out = false;
+        {
+            float high[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) high[r] = fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[0][2 + r], x[1][2 + r]) * 0.0625f) * scale2[r];
+            out = high[0] > ref[0] + kHighest || high[1] > ref[1] + kHighest;
             if (ATTEND) {
-                const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + F::kKeyTile + F::kCodeBytes) + hb * 16 + g;
-                va = vm[0], vb = vm[8];
-            }
-            if (key0 + 16 > M) {                             // rows past the count
-                if (key0 + g >= M) x[0] = x[1] = SHOTKV_NEG_INF, va = 0;
-                if (key0 + g + 8 >= M) x[2] = x[3] = SHOTKV_NEG_INF, vb = 0;
-            }
-            float y[4], sa = bf16_high(va) * unit, sb = bf16_high(vb) * unit;
+                const float s = fmaxf(fmaxf(bf16_high(va[0]), bf16_high(vb[0])), fmaxf(bf16_high(va[1]), bf16_high(vb[1])));
+                out |= !begun || s * unit >= 4.f;
+                if (__any_sync(0xffffffffu, out)) {
+                    raise(high);
+                    float m = s;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i] = x[i] - ref[i & 1];
-            bool out = fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])) > kHighest;
-            if (ATTEND) out |= !begun || fmaxf(sa, sb) >= 4.f;
-            if (__any_sync(0xffffffffu, out)) {
-                raise(x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = x[i] - ref[i & 1];
-                if (ATTEND) {
-                    float s = fmaxf(bf16_high(va), bf16_high(vb));
-#pragma unroll
-                    for (int o = 4; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
-                    const int e = min(max((int)(__float_as_uint(s) >> 23), 67), 250);      // its exponent
+                    for (int o = 4; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                    const int e = min(max((int)(__float_as_uint(m) >> 23), 67), 250);      // its exponent
                     float next = __uint_as_float((uint32_t)(254 - e) << 23);
                     if (begun) next = fminf(unit, next);
                     const float al = next / unit;
@@ -354,45 +402,74 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                         for (int c = 0; c < 4; ++c) O[mt][c] *= al;
                     unit = next;
                     begun = true;
-                    sa = bf16_high(va) * unit, sb = bf16_high(vb) * unit;
                 }
+            } else if (__any_sync(0xffffffffu, out)) {
+                raise(high);
             }
+        }
+        // weights, and with them (ATTEND) the values' scales as B fragments: high parts and remainders
+        uint32_t wh[2][2], wl[2][2];
+        const uint64_t down = tc::pack2(-ref[0], -ref[1]);
+        uint64_t zz = tc::pack2(z[0], z[1]);
+#pragma unroll
+        for (int hb = 0; hb < 2; ++hb) {
             float w[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = ex2f(y[i]);
-                z[i & 1] += w[i];
+            for (int k = 0; k < 4; k += 2) {                 // a key's two rows
+                tc::unpack2(tc::ffma2(tc::pack2(x[hb][k], x[hb][k + 1]), k ? scales16 : scales, down), w[k], w[k + 1]);
+                w[k] = ex2f(w[k]), w[k + 1] = ex2f(w[k + 1]);
+                zz = tc::fadd2(zz, tc::pack2(w[k], w[k + 1]));
             }
             if (ATTEND) {
+                const float sa = bf16_high(va[hb]) * unit, sb = bf16_high(vb[hb]) * unit, za = bf16_low(va[hb]), zb = bf16_low(vb[hb]);
                 w[0] *= sa, w[1] *= sa, w[2] *= sb, w[3] *= sb;
-                const float za = bf16_low(va), zb = bf16_low(vb);
                 wz[0] = fmaf(w[0], za, fmaf(w[2], zb, wz[0]));
                 wz[1] = fmaf(w[1], za, fmaf(w[3], zb, wz[1]));
-                const uint32_t h0 = pack_f16(w[0], w[1]), h1 = pack_f16(w[2], w[3]);
-                const float2 f0 = unpack_f16(h0), f1 = unpack_f16(h1);
-                const uint32_t bh0 = transposed(h0), bh1 = transposed(h1);
-                const uint32_t bl0 = transposed(pack_f16(w[0] - f0.x, w[1] - f0.y)), bl1 = transposed(pack_f16(w[2] - f1.x, w[3] - f1.y));
-                const uint4* vc = reinterpret_cast<const uint4*>(st + F::kKeyTile + hb * F::kHalfBytes) + lane;
 #pragma unroll
-                for (int h = 0; h < NC; ++h) {
-                    const uint4 vw = vc[h * 32];
-                    const uint32_t e[4] = {vw.x, vw.y, vw.z, vw.w};
+                for (int k = 0; k < 2; ++k) {
+                    const uint32_t h = pack_f16(w[2 * k], w[2 * k + 1]);
+                    const float2 f = unpack_f16(h);
+                    float rest0, rest1;
+                    tc::unpack2(tc::ffma2(tc::pack2(f.x, f.y), tc::pack2(-1.f, -1.f), tc::pack2(w[2 * k], w[2 * k + 1])), rest0, rest1);
+                    const uint32_t l = pack_f16(rest0, rest1);
+                    wh[hb][k] = transposed(second ? l : h);
+                    if (!PAIRED) wl[hb][k] = transposed(l);
+                }
+            }
+        }
+        tc::unpack2(zz, z[0], z[1]);
+        if (ATTEND) {
+            const uint4* vc = reinterpret_cast<const uint4*>(st + F::kKeyTile) + lane;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t a[4];
-                        codes_f16(e[i], a);
-                        mma_f16_16816(O[h * 4 + i], a, bh0, bh1);
-                        mma_f16_16816(O[h * 4 + i], a, bl0, bl1);
-                    }
+            for (int h = 0; h < NC; ++h) {
+                const uint4 v0 = vc[h * 32], v1 = vc[F::kHalfBytes / 16 + h * 32];
+                const uint32_t e0[4] = {v0.x, v0.y, v0.z, v0.w}, e1[4] = {v1.x, v1.y, v1.z, v1.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float c[4];
+                    uint32_t a[4];
+                    codes_f16(e0[i], a);
+                    if (PAIRED) mma_f16_16816_first(c, a, wh[0][0], wh[0][1]);
+                    else mma_f16_16816_first(c, a, wl[0][0], wl[0][1]), mma_f16_16816(c, a, wh[0][0], wh[0][1]);
+                    codes_f16(e1[i], a);
+                    if (!PAIRED) mma_f16_16816(c, a, wl[1][0], wl[1][1]);
+                    mma_f16_16816(c, a, wh[1][0], wh[1][1]);
+                    float(&o)[4] = O[h * 4 + i];
+                    tc::unpack2(tc::fadd2(tc::pack2(o[0], o[1]), tc::pack2(c[0], c[1])), o[0], o[1]);
+                    tc::unpack2(tc::fadd2(tc::pack2(o[2], o[3]), tc::pack2(c[2], c[3])), o[2], o[3]);
                 }
             }
         }
         __syncwarp();                                       // every lane has read the stage the next copy overwrites
-        if (tile + NS * step < tiles) fetch(tile + NS * step, stage);
-        else cp_async_commit();
-        stage = stage + 1 == NS ? 0 : stage + 1;
+        if (tile + NS * step < tiles && limit) fetch(tile + NS * step, stage);
+        advance();
     }
-    cp_async_wait<0>();
+    // what was asked for beyond the kept rows lands too, before its place is used again
+#pragma unroll 1
+    for (; tile < all_tiles && tile < first_tile + NS * step; tile += step) {
+        landed();
+        advance();
+    }
 
     // ---- the warp's rows
 #pragma unroll
@@ -414,12 +491,20 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int h = 0; h < NC; ++h) {
-                float* o = sO + warp * kPitch + (2 * t4 + r) * kOutPitch<D> + h * 64 + g * 8;
+                float* o = sO + warp * kPitch + (r0 + r) * kOutPitch<D> + h * 64 + g * 8;
                 float v[8];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[2 * i] = (O[h * 4 + i][r] + wz[r]) * back, v[2 * i + 1] = (O[h * 4 + i][2 + r] + wz[r]) * back;
-                *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
-                *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        float x = O[h * 4 + i][2 * e + r];
+                        if (PAIRED) x += __shfl_xor_sync(0xffffffffu, x, 2);
+                        v[2 * i + e] = (x + wz[r]) * back;
+                    }
+                if (!second) {
+                    *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float4*>(o + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                }
             }
     }
     __syncthreads();

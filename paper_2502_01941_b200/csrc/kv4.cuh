@@ -202,17 +202,33 @@ __global__ void __launch_bounds__(kPackThreads) compact_kv4_kernel(const uint4* 
 }
 
 // ---- codes into numbers ------------------------------------------------------------------------
-// A word's four registers of an A fragment: pairs of codes -8..7 as f16, exact.  Nibbles 0 and 4 lie under the
-// significand of 1024, nibbles 1 and 5 sixteen times higher.
+// (w & MASK) | UNDER as the one instruction it is (written out, its two constants made two of it: 289 of them a tile
+// of the decode step instead of 170).
+template <uint32_t MASK, uint32_t UNDER>
+__device__ __forceinline__ uint32_t and_or(uint32_t w) {
+    uint32_t d;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "n"(MASK), "n"(UNDER));
+    return d;
+}
+// A word's four registers of an A fragment: pairs of codes -8..7 as f16, exact.  A byte under the significand of 1024
+// is 1024 + n + 16 n', its upper nibble under that of 1032 is 1032 + 16 n': their difference is n - 8, and a sixteenth of
+// the second, less 72.5, n' - 8.  (Eight instructions a word, four of them on the pipe of the logical operations; each nibble by itself
+// under 1024 takes nine and five.)
 __device__ __forceinline__ void codes_f16(uint32_t w, uint32_t (&a)[4]) {
     const auto h = [](uint32_t x) { return *reinterpret_cast<const __half2*>(&x); };
     const auto u = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
-    const __half2 low = h(0xe408e408u), sixteenth = h(0x2c002c00u), high = h(0xd480d480u);    // -1032, 1/16, -72
+    const __half2 sixteenth = h(0x2c002c00u), less = h(0xd488d488u);      // 1/16, -72.5
+    const uint32_t low = and_or<0x00ff00ffu, 0x64006400u>(w), high = __byte_perm(w, 0x64646464u, 0x4341);
+    const uint32_t low1 = and_or<0x00f000f0u, 0x64086408u>(w), high1 = and_or<0x00f000f0u, 0x64086408u>(high);
+    a[0] = u(__hsub2(h(low), h(low1)));
+    a[1] = u(__hfma2(h(low1), sixteenth, less));
+    a[2] = u(__hsub2(h(high), h(high1)));
+    a[3] = u(__hfma2(h(high1), sixteenth, less));
+}
+// The same as f16 subnormals: code + 8 in units of 2^-24, of registers 1 and 3 (rows g + 8 of a product) of 2^-20.
+__device__ __forceinline__ void codes_subnormal(uint32_t w, uint32_t (&a)[4]) {
     const uint32_t v = w >> 8;
-    a[0] = u(__hadd2(h((w & 0x000f000fu) | 0x64006400u), low));
-    a[1] = u(__hfma2(h((w & 0x00f000f0u) | 0x64006400u), sixteenth, high));
-    a[2] = u(__hadd2(h((v & 0x000f000fu) | 0x64006400u), low));
-    a[3] = u(__hfma2(h((v & 0x00f000f0u) | 0x64006400u), sixteenth, high));
+    a[0] = w & 0x000f000fu, a[1] = w & 0x00f000f0u, a[2] = v & 0x000f000fu, a[3] = v & 0x00f000f0u;
 }
 
 // The packed rows below the count as bf16, each element rounded once: a warp takes 16 rows, as above.

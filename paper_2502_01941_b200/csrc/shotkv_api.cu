@@ -109,7 +109,7 @@ struct shotkv_ctx {
     int32_t* static_offsets = nullptr;         // device address of the built-in boundary table (looked up on first use)
     void* encode_tiled = nullptr;              // cuTensorMapEncodeTiled, resolved at creation
     DecodeRoom room_attend[2][2], room_score[2][2];   // [d = 128][the step ends in its first kernel] (asked at creation)
-    DecodeRoom room_kv4[2][2][2];              // [d = 128][with the attention output][the step ends in its first kernel]
+    DecodeRoom room_kv4[2][3][2];              // [d = 128][scores, with the attention output, the same in pairs][ended there]
     int whole_score[2][2] = {};                // CTAs that have a unit each and fit an SM, two and four blocks of keys deep
 };
 
@@ -827,10 +827,16 @@ cudaError_t set_kernel_attributes() {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     };
-    const void* kv4[] = {(const void*)decode_kv4_kernel<128, true, false>,  (const void*)decode_kv4_kernel<128, true, true>,
-                         (const void*)decode_kv4_kernel<64, true, false>,   (const void*)decode_kv4_kernel<64, true, true>,
-                         (const void*)decode_kv4_kernel<128, false, false>, (const void*)decode_kv4_kernel<128, false, true>,
-                         (const void*)decode_kv4_kernel<64, false, false>,  (const void*)decode_kv4_kernel<64, false, true>};
+    std::vector<const void*> kv4;
+    const auto kv4_forms = [&](auto d) {
+        constexpr int D = decltype(d)::value;
+        for (const void* f : {(const void*)decode_kv4_kernel<D, true, false, false>, (const void*)decode_kv4_kernel<D, true, true, false>,
+                              (const void*)decode_kv4_kernel<D, true, false, true>, (const void*)decode_kv4_kernel<D, true, true, true>,
+                              (const void*)decode_kv4_kernel<D, false, false, false>, (const void*)decode_kv4_kernel<D, false, true, false>})
+            kv4.push_back(f);
+    };
+    kv4_forms(std::integral_constant<int, 64>());
+    kv4_forms(std::integral_constant<int, 128>());
     for (const void* f : attend) in_clusters(f);
     for (const void* f : score) in_clusters(f);
     for (const void* f : kv4) in_clusters(f);
@@ -878,10 +884,15 @@ cudaError_t ask_decode_room_t(shotkv_ctx* ctx) {
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, false, kDeep>, 256, score[0]);
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, true, kDeep>, 256, score[1]);
     DecodeRoom(*kv4)[2] = ctx->room_kv4[D == 128];
-    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, false, false>, StepKv4<D, false>::kWarps * 32, kv4[0][0]);
-    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, false, true>, StepKv4<D, false>::kWarps * 32, kv4[0][1]);
-    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, true, false>, StepKv4<D, true>::kWarps * 32, kv4[1][0]);
-    if (e == cudaSuccess) e = ask_room(decode_kv4_kernel<D, true, true>, StepKv4<D, true>::kWarps * 32, kv4[1][1]);
+    const auto room_of = [&](auto* kernel, DecodeRoom& room) {
+        if (e == cudaSuccess) e = ask_room(kernel, StepKv4<D, true>::kWarps * 32, room);
+    };
+    room_of(decode_kv4_kernel<D, false, false, false>, kv4[0][0]);
+    room_of(decode_kv4_kernel<D, false, true, false>, kv4[0][1]);
+    room_of(decode_kv4_kernel<D, true, false, false>, kv4[1][0]);
+    room_of(decode_kv4_kernel<D, true, true, false>, kv4[1][1]);
+    room_of(decode_kv4_kernel<D, true, false, true>, kv4[2][0]);
+    room_of(decode_kv4_kernel<D, true, true, true>, kv4[2][1]);
     int* whole = ctx->whole_score[D == 128];
     const auto fit = [&](int& ctas, auto* kernel) {
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, 256, 0);
@@ -1610,26 +1621,27 @@ int launch_decode_score(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishPara
 }
 
 // The same over a prompt in 4 bits.
-template <int D, bool ATTEND>
+template <int D, bool ATTEND, bool PAIRED>
 int launch_decode_kv4_t(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
                         cudaStream_t stream) {
     constexpr int threads = StepKv4<D, ATTEND>::kWarps * 32;
-    const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND];
+    const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND + PAIRED];
     const auto smem_of = [&](int n) { return kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, n); };
     p.nsplit = decode_split(room[0], smem_of, U, (long long)p.Mcap + p.n_old + 1, StepKv4<D, ATTEND>::kWarps, kLeastKv4);
     const size_t smem = smem_of(p.nsplit), end = fused_end_smem_bytes(p.Hkv, f.n, f.k < f.n);
     const dim3 grid(U * p.nsplit);
     ended = smem + end <= kBigSmem &&
             ends_fused(ctx, room[1].with(smem + end), p, f, U, threads, ATTEND ? kFusedEntriesAttend : kFusedEntriesScore);
-    if (ended) return launch(ctx, decode_kv4_kernel<D, ATTEND, true>, grid, threads, smem + end, stream, p.Hkv * p.nsplit, kEarly, p, f, cache);
+    if (ended) return launch(ctx, decode_kv4_kernel<D, ATTEND, true, PAIRED>, grid, threads, smem + end, stream, p.Hkv * p.nsplit, kEarly, p, f, cache);
     if (smem > kBigSmem) return fail(ctx, SHOTKV_ERR_UNSUPPORTED_SHAPE, "Dcap too large for the step over a packed cache");
-    return launch(ctx, decode_kv4_kernel<D, ATTEND, false>, grid, threads, smem, stream, p.nsplit, kEarly, p, f, cache);
+    return launch(ctx, decode_kv4_kernel<D, ATTEND, false, PAIRED>, grid, threads, smem, stream, p.nsplit, kEarly, p, f, cache);
 }
-int launch_decode_kv4(shotkv_ctx* ctx, int d, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
+template <int D>
+int launch_decode_kv4(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
                       cudaStream_t stream) {
-    const auto run = p.out ? (d == 128 ? launch_decode_kv4_t<128, true> : launch_decode_kv4_t<64, true>)
-                           : (d == 128 ? launch_decode_kv4_t<128, false> : launch_decode_kv4_t<64, false>);
-    return run(ctx, p, f, cache, U, ended, stream);
+    if (!p.out) return launch_decode_kv4_t<D, false, false>(ctx, p, f, cache, U, ended, stream);
+    return p.G <= 4 ? launch_decode_kv4_t<D, true, true>(ctx, p, f, cache, U, ended, stream)
+                    : launch_decode_kv4_t<D, true, false>(ctx, p, f, cache, U, ended, stream);
 }
 
 // One decode step; with `attn_out` the score kernel is the variant that also writes the attention output.  `packed`: Kc and Vc
@@ -1677,7 +1689,8 @@ int decode_step_impl(shotkv_ctx* ctx, shotkv_decode_state* st, const shotkv_bf16
     prof_begin(ctx);
     prof_mark(ctx, stream);
     if (packed) {
-        rc = launch_decode_kv4(ctx, d.d, p, f, PackedCache{(const unsigned char*)Kc, (const unsigned char*)Vc}, U, ended, stream);
+        const PackedCache cache{(const unsigned char*)Kc, (const unsigned char*)Vc};
+        rc = d.d == 128 ? launch_decode_kv4<128>(ctx, p, f, cache, U, ended, stream) : launch_decode_kv4<64>(ctx, p, f, cache, U, ended, stream);
     } else {
         const auto first = attn_out ? (d.d == 128 ? launch_decode_attend<128> : launch_decode_attend<64>)
                                     : (d.d == 128 ? launch_decode_score<128> : launch_decode_score<64>);
