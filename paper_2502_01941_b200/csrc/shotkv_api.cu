@@ -1232,15 +1232,17 @@ int shotkv_norm_rope(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_rope
     // of the queries all rows, or those in the window
     const int to_window = dims->N - dims->W - rope->first;
     p.q_first = q_out || to_window < 0 ? 0 : std::min(to_window, (int)rope->rows);
-    const int section = kRopeAhead * 256 / dims->d;
-    p.kv_sections = (dims->Hkv + section - 1) / section;
-    p.q_sections = (dims->H + section - 1) / section;
-    const long long kv = 2LL * dims->B * rope->rows * p.kv_sections, items = kv + (long long)dims->B * (rope->rows - p.q_first) * p.q_sections;
-    if (items > 0x7fffff00LL) return fail(ctx, SHOTKV_ERR_UNSUPPORTED_SHAPE, "B * rows * heads too large");
-    p.kv_items = (int)kv;
-    p.items = (int)items;
-    constexpr int warps = kRopeThreads / 32;
-    return launch(ctx, dims->d == 128 ? norm_rope_kernel<128> : norm_rope_kernel<64>, dim3((p.items + warps - 1) / warps), kRopeThreads, 0,
+    const auto ctas = [&](int heads, int rows, int ahead, int& vectors, int& sections) -> long long {
+        if (dims->d == 128) rope_share<128>(heads, ahead, vectors, sections);
+        else rope_share<64>(heads, ahead, vectors, sections);
+        const long long warps = (long long)((rows + ahead / vectors - 1) / (ahead / vectors)) * sections;
+        return (warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+    };
+    const long long kv = ctas(dims->Hkv, rope->rows, kRopeAhead, p.kv_vectors, p.kv_sections);
+    const long long grid = kv + ctas(dims->H, rope->rows - p.q_first, 2 * kRopeAhead, p.q_vectors, p.q_sections);
+    if (grid > 0x7fffffLL || dims->B > 65535) return fail(ctx, SHOTKV_ERR_UNSUPPORTED_SHAPE, "rows * heads too large, or B > 65535");
+    p.kv_ctas = (int)kv;
+    return launch(ctx, dims->d == 128 ? norm_rope_kernel<128> : norm_rope_kernel<64>, dim3((unsigned)grid, dims->B), kRopeThreads, 0,
                   (cudaStream_t)stream_, 1, kEarly, p);
 }
 
