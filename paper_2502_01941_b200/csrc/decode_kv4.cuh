@@ -41,6 +41,14 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  : "memory");
 }
 
+// Operand columns 0 .. 3 are one number of every key, columns 4 .. 7 another, and the lanes of columns 0 .. 3 have both of keys 0 .. 7, those of
+// columns 4 .. 7 (`second`) of keys 8 .. 15: what each contributes to the two 8 x 8 matrices.
+__device__ __forceinline__ void halves_of_columns(uint32_t one, uint32_t another, bool second, uint32_t& keys0, uint32_t& keys8) {
+    const uint32_t other = __shfl_xor_sync(0xffffffffu, second ? one : another, 2);
+    keys0 = second ? other : one;
+    keys8 = second ? another : other;
+}
+
 struct PackedCache {
     const unsigned char *K4, *V4;            // [U][tiles][Kv4 tile]
 };
@@ -133,6 +141,10 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     // an operand is g, and of an accumulator 2*t4 and 2*t4 + 1, which are rows r0 and r0 + 1.
     const int g_row = PAIRED ? g & 3 : g, r0 = PAIRED ? (2 * t4) & 3 : 2 * t4;
     const bool second = PAIRED && t4 >= 2;                   // the columns of the weights' remainders
+    // Of the 16 keys of an accumulator a lane has keys g and g + 8, and both in both columns of a row where there are two: it
+    // goes on with the first or the second of them then (with both in all lanes, a tenth more instructions).
+    constexpr int KL = PAIRED ? 1 : 2;
+    const auto key_of = [&](int k) { return g + (k || second ? 8 : 0); };
     const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bl * p.H + (size_t)hk * p.G + g_row) * D);
     uint4 qf[NB];
 #pragma unroll
@@ -212,12 +224,13 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         for (int c = 0; c < 4; ++c) O[mt][c] = 0.f;
     // of query rows 2*t4 and 2*t4 + 1: the reference (the same in the 8 lanes of a t4), this lane's part of the sum of p, and of w z_v
     float ref[2] = {kUnset, kUnset}, z[2] = {0.f, 0.f}, wz[2] = {0.f, 0.f};
+    constexpr int kFirstLane = PAIRED ? 2 : 4;               // lanes a row's keys are spread over: those of one t4, or of t4 and t4 ^ 2
     const auto raise = [&](const float (&high)[2]) {         // new references, from all lanes' greatest logits
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             float m = high[r];
 #pragma unroll
-            for (int o = 4; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            for (int o = kFirstLane; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
             const float up = fmaxf(ref[r], m - kLift);
             const float al = ex2f(ref[r] - up);
             ref[r] = up;
@@ -252,34 +265,38 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                 mma_bf16_16816(c, f1, q.z, q.w);
             }
         }
-        float x[4];
+        float x[2 * KL];                                     // of this lane's keys, each its two rows
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = base + g + 8 * (i >> 1), r = r0 + (i & 1);
-            x[i] = j < n ? c[i] * p.scale_log2 : SHOTKV_NEG_INF;
-            if (j < n && r < p.G && !second) sdec[r * p.Dcap + j] = x[i];
+        for (int i = 0; i < 2 * KL; ++i) {
+            const int j = base + key_of(i >> 1), r = r0 + (i & 1);
+            x[i] = j < n ? (second ? c[2 + (i & 1)] : c[i]) * p.scale_log2 : SHOTKV_NEG_INF;
+            if (j < n && r < p.G) sdec[r * p.Dcap + j] = x[i];
         }
-        const float high[2] = {fmaxf(x[0], x[2]), fmaxf(x[1], x[3])};
+        const float high[2] = {fmaxf(x[0], x[2 * KL - 2]), fmaxf(x[1], x[2 * KL - 1])};
         if (__any_sync(0xffffffffu, high[0] > ref[0] + kHighest || high[1] > ref[1] + kHighest)) raise(high);
-        float w[4];
+        float w[2 * KL];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 2 * KL; ++i) {
             w[i] = ex2f(x[i] - ref[i & 1]);
             z[i & 1] += w[i];
         }
         if (ATTEND) {
             // weights as B fragments in three bf16 parts (2^-24), keys in their order on the product's inner side; paired, the
-            // first two are one fragment
+            // first two are the columns of one fragment
             constexpr int PARTS = PAIRED ? 2 : 3;
             uint32_t b0[3], b1[3];
 #pragma unroll
-            for (int s = 0; s < 3; ++s) {
-                b0[s] = pack_bf16(w[0], w[1]), b1[s] = pack_bf16(w[2], w[3]);
-                w[0] -= bf16_low(b0[s]), w[1] -= bf16_high(b0[s]), w[2] -= bf16_low(b1[s]), w[3] -= bf16_high(b1[s]);
-            }
-            if (PAIRED) {
-                b0[0] = second ? b0[1] : b0[0], b1[0] = second ? b1[1] : b1[0];
-                b0[1] = second ? 0u : b0[2], b1[1] = second ? 0u : b1[2];
+            for (int s = 0; s < 3; ++s)
+#pragma unroll
+                for (int k = 0; k < KL; ++k) {
+                    uint32_t& b = k ? b1[s] : b0[s];
+                    b = pack_bf16(w[2 * k], w[2 * k + 1]);
+                    w[2 * k] -= bf16_low(b), w[2 * k + 1] -= bf16_high(b);
+                }
+            if constexpr (PAIRED) {
+                const uint32_t l = b0[2], other = __shfl_xor_sync(0xffffffffu, l, 2);
+                halves_of_columns(b0[0], b0[1], second, b0[0], b1[0]);
+                b0[1] = second ? 0u : l, b1[1] = second ? 0u : other;
             }
 #pragma unroll
             for (int s = 0; s < PARTS; ++s) b0[s] = transposed(b0[s]), b1[s] = transposed(b1[s]);
@@ -307,7 +324,13 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 
     // ---- packed rows
     const int M = min(kept, p.Mcap), tiles = kv4_tiles(M);
-    const uint64_t scales = tc::pack2(scale2[0], scale2[1]), scales16 = tc::pack2(scale2[0] * 0.0625f, scale2[1] * 0.0625f);
+    // what is left of the factors of codes_subnormal for this lane's keys: c + 8 is multiplied, and of key g + 8 sixteen times that
+    float ease[KL], z_by[KL], z_less[KL];
+#pragma unroll
+    for (int k = 0; k < KL; ++k) {
+        const bool high = k || second;
+        ease[k] = high ? 0.0625f : 1.f, z_by[k] = high ? 16.f : 1.f, z_less[k] = high ? -128.f : -8.f;
+    }
     float unit = 1.f;                                        // O and wz are in units of 1 / unit
     bool begun = false;
     int stage = 0;
@@ -326,24 +349,24 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     for (; tile < tiles; tile += step) {
         landed();
         const unsigned char* st = mine + stage * Cfg::kStageBytes;
-        // of the tile's halves hb: keys 16 hb + g (x[hb][0..1]: rows 2*t4, 2*t4 + 1) and 16 hb + g + 8 (x[hb][2..3])
-        float x[2][4] = {};
-        uint32_t va[2], vb[2];                               // the values' words of these rows
+        // of the tile's halves hb: this lane's keys' two rows (still with `ease` to come), and words of the values
+        float x[2][2 * KL] = {};
+        uint32_t vw[2][KL];
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
             const uint4* kc = reinterpret_cast<const uint4*>(st + hb * F::kHalfBytes) + lane;
-            const uint32_t* km = reinterpret_cast<const uint32_t*>(st + F::kCodeBytes) + (hb * 16 + g) * NB;
-            uint32_t ma[NB], mb[NB];
-            if constexpr (NB == 4) {
-                const uint4 a = *reinterpret_cast<const uint4*>(km), b = *reinterpret_cast<const uint4*>(km + 8 * NB);
-                ma[0] = a.x, ma[1] = a.y, ma[2] = a.z, ma[3] = a.w, mb[0] = b.x, mb[1] = b.y, mb[2] = b.z, mb[3] = b.w;
-            } else {
-                const uint2 a = *reinterpret_cast<const uint2*>(km), b = *reinterpret_cast<const uint2*>(km + 8 * NB);
-                ma[0] = a.x, ma[1] = a.y, mb[0] = b.x, mb[1] = b.y;
-            }
-            if (ATTEND) {
-                const uint32_t* vm = reinterpret_cast<const uint32_t*>(st + F::kKeyTile + F::kCodeBytes) + hb * 16 + g;
-                va[hb] = vm[0], vb[hb] = vm[8];
+            uint32_t m[KL][NB];
+#pragma unroll
+            for (int k = 0; k < KL; ++k) {
+                const uint32_t* km = reinterpret_cast<const uint32_t*>(st + F::kCodeBytes) + (hb * 16 + key_of(k)) * NB;
+                if constexpr (NB == 4) {
+                    const uint4 a = *reinterpret_cast<const uint4*>(km);
+                    m[k][0] = a.x, m[k][1] = a.y, m[k][2] = a.z, m[k][3] = a.w;
+                } else {
+                    const uint2 a = *reinterpret_cast<const uint2*>(km);
+                    m[k][0] = a.x, m[k][1] = a.y;
+                }
+                if (ATTEND) vw[hb][k] = reinterpret_cast<const uint32_t*>(st + F::kKeyTile + F::kCodeBytes)[hb * 16 + key_of(k)];
             }
 #pragma unroll
             for (int h = 0; h < NC; ++h) {
@@ -359,38 +382,41 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     mma_f16_16816_first(c, a, q.x, q.y);
                     codes_subnormal(i ? kw.w : kw.y, a);
                     mma_f16_16816(c, a, q.z, q.w);
-                    // c + 8 was multiplied, and of key g + 8 sixteen times that, as which its logits remain for now
-                    const float sa = bf16_high(ma[kb]), za = bf16_low(ma[kb]) - 8.f;
-                    const float sb = bf16_high(mb[kb]), zb = fmaf(bf16_low(mb[kb]), 16.f, -128.f);
-                    x[hb][0] = fmaf(sa, fmaf(za, qsum.x, c[0]), x[hb][0]);
-                    x[hb][1] = fmaf(sa, fmaf(za, qsum.y, c[1]), x[hb][1]);
-                    x[hb][2] = fmaf(sb, fmaf(zb, qsum.x, c[2]), x[hb][2]);
-                    x[hb][3] = fmaf(sb, fmaf(zb, qsum.y, c[3]), x[hb][3]);
+                    if (PAIRED) c[0] = second ? c[2] : c[0], c[1] = second ? c[3] : c[1];
+#pragma unroll
+                    for (int k = 0; k < KL; ++k) {
+                        const float s = bf16_high(m[k][kb]), zs = fmaf(bf16_low(m[k][kb]), z_by[k], z_less[k]);
+                        x[hb][2 * k] = fmaf(s, fmaf(zs, qsum.x, c[2 * k]), x[hb][2 * k]);
+                        x[hb][2 * k + 1] = fmaf(s, fmaf(zs, qsum.y, c[2 * k + 1]), x[hb][2 * k + 1]);
+                    }
                 }
             }
         }
         if (tile * 32 + 32 > M)                              // rows past the count
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb) {
-                const int key = tile * 32 + hb * 16 + g;
-                if (key >= M) x[hb][0] = x[hb][1] = SHOTKV_NEG_INF, va[hb] = 0;
-                if (key + 8 >= M) x[hb][2] = x[hb][3] = SHOTKV_NEG_INF, vb[hb] = 0;
-            }
+            for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                for (int k = 0; k < KL; ++k)
+                    if (tile * 32 + hb * 16 + key_of(k) >= M) x[hb][2 * k] = x[hb][2 * k + 1] = SHOTKV_NEG_INF, vw[hb][k] = 0;
         bool out = false;
         {
             float high[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) high[r] = fmaxf(fmaxf(x[0][r], x[1][r]), fmaxf(x[0][2 + r], x[1][2 + r]) * 0.0625f) * scale2[r];
+            for (int r = 0; r < 2; ++r) {
+                high[r] = fmaxf(x[0][r], x[1][r]) * ease[0];
+                if (KL == 2) high[r] = fmaxf(high[r], fmaxf(x[0][2 * KL - 2 + r], x[1][2 * KL - 2 + r]) * ease[KL - 1]);
+                high[r] *= scale2[r];
+            }
             out = high[0] > ref[0] + kHighest || high[1] > ref[1] + kHighest;
             if (ATTEND) {
-                const float s = fmaxf(fmaxf(bf16_high(va[0]), bf16_high(vb[0])), fmaxf(bf16_high(va[1]), bf16_high(vb[1])));
+                float s = fmaxf(bf16_high(vw[0][0]), bf16_high(vw[1][0]));
+                if (KL == 2) s = fmaxf(s, fmaxf(bf16_high(vw[0][KL - 1]), bf16_high(vw[1][KL - 1])));
                 out |= !begun || s * unit >= 4.f;
                 if (__any_sync(0xffffffffu, out)) {
                     raise(high);
-                    float m = s;
 #pragma unroll
-                    for (int o = 4; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                    const int e = min(max((int)(__float_as_uint(m) >> 23), 67), 250);      // its exponent
+                    for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
+                    const int e = min(max((int)(__float_as_uint(s) >> 23), 67), 250);      // its exponent
                     float next = __uint_as_float((uint32_t)(254 - e) << 23);
                     if (begun) next = fminf(unit, next);
                     const float al = next / unit;
@@ -413,28 +439,32 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         uint64_t zz = tc::pack2(z[0], z[1]);
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
-            float w[4];
+            uint32_t hi[KL], lo[KL];
 #pragma unroll
-            for (int k = 0; k < 4; k += 2) {                 // a key's two rows
-                tc::unpack2(tc::ffma2(tc::pack2(x[hb][k], x[hb][k + 1]), k ? scales16 : scales, down), w[k], w[k + 1]);
-                w[k] = ex2f(w[k]), w[k + 1] = ex2f(w[k + 1]);
-                zz = tc::fadd2(zz, tc::pack2(w[k], w[k + 1]));
-            }
-            if (ATTEND) {
-                const float sa = bf16_high(va[hb]) * unit, sb = bf16_high(vb[hb]) * unit, za = bf16_low(va[hb]), zb = bf16_low(vb[hb]);
-                w[0] *= sa, w[1] *= sa, w[2] *= sb, w[3] *= sb;
-                wz[0] = fmaf(w[0], za, fmaf(w[2], zb, wz[0]));
-                wz[1] = fmaf(w[1], za, fmaf(w[3], zb, wz[1]));
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t h = pack_f16(w[2 * k], w[2 * k + 1]);
-                    const float2 f = unpack_f16(h);
-                    float rest0, rest1;
-                    tc::unpack2(tc::ffma2(tc::pack2(f.x, f.y), tc::pack2(-1.f, -1.f), tc::pack2(w[2 * k], w[2 * k + 1])), rest0, rest1);
-                    const uint32_t l = pack_f16(rest0, rest1);
-                    wh[hb][k] = transposed(second ? l : h);
-                    if (!PAIRED) wl[hb][k] = transposed(l);
+            for (int k = 0; k < KL; ++k) {
+                float w[2];
+                const uint64_t scales = tc::pack2(scale2[0] * ease[k], scale2[1] * ease[k]);
+                tc::unpack2(tc::ffma2(tc::pack2(x[hb][2 * k], x[hb][2 * k + 1]), scales, down), w[0], w[1]);
+                w[0] = ex2f(w[0]), w[1] = ex2f(w[1]);
+                zz = tc::fadd2(zz, tc::pack2(w[0], w[1]));
+                if (ATTEND) {
+                    const float s = bf16_high(vw[hb][k]) * unit, zs = bf16_low(vw[hb][k]);
+                    w[0] *= s, w[1] *= s;
+                    wz[0] = fmaf(w[0], zs, wz[0]);
+                    wz[1] = fmaf(w[1], zs, wz[1]);
+                    hi[k] = pack_f16(w[0], w[1]);
+                    const float2 f = unpack_f16(hi[k]);
+                    float rest[2];
+                    tc::unpack2(tc::ffma2(tc::pack2(f.x, f.y), tc::pack2(-1.f, -1.f), tc::pack2(w[0], w[1])), rest[0], rest[1]);
+                    lo[k] = pack_f16(rest[0], rest[1]);
                 }
+            }
+            if constexpr (ATTEND && PAIRED) {
+                halves_of_columns(hi[0], lo[0], second, wh[hb][0], wh[hb][1]);
+                wh[hb][0] = transposed(wh[hb][0]), wh[hb][1] = transposed(wh[hb][1]);
+            } else if constexpr (ATTEND) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) wh[hb][k] = transposed(hi[k]), wl[hb][k] = transposed(lo[k]);
             }
         }
         tc::unpack2(zz, z[0], z[1]);
@@ -475,7 +505,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 #pragma unroll
     for (int r = 0; r < 2; ++r)
 #pragma unroll
-        for (int o = 4; o <= 16; o <<= 1) {
+        for (int o = kFirstLane; o <= 16; o <<= 1) {
             z[r] += __shfl_xor_sync(0xffffffffu, z[r], o);
             if (ATTEND) wz[r] += __shfl_xor_sync(0xffffffffu, wz[r], o);
         }

@@ -109,7 +109,7 @@ struct shotkv_ctx {
     int32_t* static_offsets = nullptr;         // device address of the built-in boundary table (looked up on first use)
     void* encode_tiled = nullptr;              // cuTensorMapEncodeTiled, resolved at creation
     DecodeRoom room_attend[2][2], room_score[2][2];   // [d = 128][the step ends in its first kernel] (asked at creation)
-    DecodeRoom room_kv4[2][3][2];              // [d = 128][scores, with the attention output, the same in pairs][ended there]
+    DecodeRoom room_kv4[2][2][2][2];           // [d = 128][with the attention output][paired][the step ends in its first kernel]
     int whole_score[2][2] = {};                // CTAs that have a unit each and fit an SM, two and four blocks of keys deep
 };
 
@@ -832,7 +832,8 @@ cudaError_t set_kernel_attributes() {
         constexpr int D = decltype(d)::value;
         for (const void* f : {(const void*)decode_kv4_kernel<D, true, false, false>, (const void*)decode_kv4_kernel<D, true, true, false>,
                               (const void*)decode_kv4_kernel<D, true, false, true>, (const void*)decode_kv4_kernel<D, true, true, true>,
-                              (const void*)decode_kv4_kernel<D, false, false, false>, (const void*)decode_kv4_kernel<D, false, true, false>})
+                              (const void*)decode_kv4_kernel<D, false, false, false>, (const void*)decode_kv4_kernel<D, false, true, false>,
+                              (const void*)decode_kv4_kernel<D, false, false, true>, (const void*)decode_kv4_kernel<D, false, true, true>})
             kv4.push_back(f);
     };
     kv4_forms(std::integral_constant<int, 64>());
@@ -883,16 +884,17 @@ cudaError_t ask_decode_room_t(shotkv_ctx* ctx) {
     if (e == cudaSuccess) e = ask_room(decode_attend_kernel<D, true>, AttendCfg<D>::kWarps * 32, attend[1]);
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, false, kDeep>, 256, score[0]);
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, true, kDeep>, 256, score[1]);
-    DecodeRoom(*kv4)[2] = ctx->room_kv4[D == 128];
-    const auto room_of = [&](auto* kernel, DecodeRoom& room) {
-        if (e == cudaSuccess) e = ask_room(kernel, StepKv4<D, true>::kWarps * 32, room);
+    const auto room_of = [&](auto* kernel, bool attend, bool paired, bool fused) {
+        if (e == cudaSuccess) e = ask_room(kernel, StepKv4<D, true>::kWarps * 32, ctx->room_kv4[D == 128][attend][paired][fused]);
     };
-    room_of(decode_kv4_kernel<D, false, false, false>, kv4[0][0]);
-    room_of(decode_kv4_kernel<D, false, true, false>, kv4[0][1]);
-    room_of(decode_kv4_kernel<D, true, false, false>, kv4[1][0]);
-    room_of(decode_kv4_kernel<D, true, true, false>, kv4[1][1]);
-    room_of(decode_kv4_kernel<D, true, false, true>, kv4[2][0]);
-    room_of(decode_kv4_kernel<D, true, true, true>, kv4[2][1]);
+    room_of(decode_kv4_kernel<D, false, false, false>, false, false, false);
+    room_of(decode_kv4_kernel<D, false, true, false>, false, false, true);
+    room_of(decode_kv4_kernel<D, false, false, true>, false, true, false);
+    room_of(decode_kv4_kernel<D, false, true, true>, false, true, true);
+    room_of(decode_kv4_kernel<D, true, false, false>, true, false, false);
+    room_of(decode_kv4_kernel<D, true, true, false>, true, false, true);
+    room_of(decode_kv4_kernel<D, true, false, true>, true, true, false);
+    room_of(decode_kv4_kernel<D, true, true, true>, true, true, true);
     int* whole = ctx->whole_score[D == 128];
     const auto fit = [&](int& ctas, auto* kernel) {
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, 256, 0);
@@ -1539,7 +1541,7 @@ namespace {
 // 2, 185 keys 8.5 -> 7.1; 1 block: 8 heads of 1,150 keys 7.0 -> 7.3).  Scores alone take less per block than a larger
 // cluster costs (8 heads of 3,400 keys 5.3 us with 2.5 blocks, 6.1 with 2, 5.7 with 3; with 2.5, 1 to 148 units of 64
 // to 8,192 keys all take what they took with 2 and at most eight CTAs, within 2 %, or less).
-constexpr int kLeastAttend = 8, kLeastScore = 15, kLeastKv4 = 12;
+constexpr int kLeastAttend = 8, kLeastScore = 15, kLeastKv4 = 8;
 template <class Smem>
 int decode_split(const DecodeRoom& room, Smem&& smem, long long U, long long keys, int warps, int least) {
     int n = kMaxSplit;
@@ -1627,7 +1629,7 @@ template <int D, bool ATTEND, bool PAIRED>
 int launch_decode_kv4_t(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
                         cudaStream_t stream) {
     constexpr int threads = StepKv4<D, ATTEND>::kWarps * 32;
-    const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND + PAIRED];
+    const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND][PAIRED];
     const auto smem_of = [&](int n) { return kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, n); };
     p.nsplit = decode_split(room[0], smem_of, U, (long long)p.Mcap + p.n_old + 1, StepKv4<D, ATTEND>::kWarps, kLeastKv4);
     const size_t smem = smem_of(p.nsplit), end = fused_end_smem_bytes(p.Hkv, f.n, f.k < f.n);
@@ -1641,9 +1643,9 @@ int launch_decode_kv4_t(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishPara
 template <int D>
 int launch_decode_kv4(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
                       cudaStream_t stream) {
-    if (!p.out) return launch_decode_kv4_t<D, false, false>(ctx, p, f, cache, U, ended, stream);
-    return p.G <= 4 ? launch_decode_kv4_t<D, true, true>(ctx, p, f, cache, U, ended, stream)
-                    : launch_decode_kv4_t<D, true, false>(ctx, p, f, cache, U, ended, stream);
+    const auto run = p.out ? (p.G <= 4 ? launch_decode_kv4_t<D, true, true> : launch_decode_kv4_t<D, true, false>)
+                           : (p.G <= 4 ? launch_decode_kv4_t<D, false, true> : launch_decode_kv4_t<D, false, false>);
+    return run(ctx, p, f, cache, U, ended, stream);
 }
 
 // One decode step; with `attn_out` the score kernel is the variant that also writes the attention output.  `packed`: Kc and Vc
