@@ -131,8 +131,8 @@ def lib() -> C.CDLL:
     if m is not None:
         m.init(Dims, Policy, DecodeState, Rope, *(C.cast(getattr(L, n), vp).value for n in (
             "shotkv_prefill_score", "shotkv_select_shots", "shotkv_compact_kv", "shotkv_prefill_compress",
-            "shotkv_decode_step", "shotkv_decode_step_attend", "shotkv_norm_rope", "shotkv_compact_kv4", "shotkv_decode_step_kv4",
-            "shotkv_decode_step_attend_kv4")))
+            "shotkv_decode_step", "shotkv_decode_step_attend", "shotkv_norm_rope", "shotkv_compact_kv4", "shotkv_unpack_kv4",
+            "shotkv_decode_step_kv4", "shotkv_decode_step_attend_kv4")))
         _native = m
     _lib = L
     return L
@@ -513,6 +513,10 @@ def shotkv_compact_kv4(ctx: Context, dims: Dims, K, V, kept_idx, kept_count, Mca
 
 
 def shotkv_unpack_kv4(ctx: Context, dims: Dims, K4, V4, kept_count, Mcap: int, Kc, Vc, stream=None) -> int:
+    if _native is not None:
+        rc = _native.unpack_kv4(ctx._h, dims, K4, V4, kept_count, Mcap, Kc, Vc, stream)
+        if rc is not None:
+            return ctx.check(rc)
     rc = lib().shotkv_unpack_kv4(ctx._h, C.byref(dims), _dev(K4, _U8, "K4"), _dev(V4, _U8, "V4"), _dev(kept_count, _I32, "kept_count"),
                                  int(Mcap), _dev(Kc, _BF16, "Kc"), _dev(Vc, _BF16, "Vc"), _stream(stream))
     return ctx.check(rc)

@@ -335,19 +335,23 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     bool begun = false;
     int stage = 0;
     uint32_t parity = 0;
-    long long limit = p.wait_cycles;                         // 0 once a wait gave up: what is there is computed with, nothing is asked for
-    const auto landed = [&] {
-        if (!tc::mbar_try(smem_u32(bars + stage), parity) && !await_messages(bars + stage, p.err, limit, parity)) limit = 0;
-        __syncwarp();
+    // The same answer in all lanes; `limit` cycles at most.
+    const auto landed = [&](long long limit) {
+        bool there = tc::mbar_try(smem_u32(bars + stage), parity);
+        if (__all_sync(0xffffffffu, there)) return true;
+        there = there || await_messages(bars + stage, p.err, limit, parity);
+        return (bool)__all_sync(0xffffffffu, there);
     };
     const auto advance = [&] {
         stage = stage + 1 == NS ? 0 : stage + 1;
         if (stage == 0) parity ^= 1;
     };
     int tile = first_tile;
+    bool lost = false;                                       // a wait gave up: the warp goes on with what it has
 #pragma unroll 1
     for (; tile < tiles; tile += step) {
-        landed();
+        lost = !landed(p.wait_cycles);
+        if (lost) break;
         const unsigned char* st = mine + stage * Cfg::kStageBytes;
         // of the tile's halves hb: this lane's keys' two rows (still with `ease` to come), and words of the values
         float x[2][2 * KL] = {};
@@ -491,15 +495,17 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             }
         }
         __syncwarp();                                       // every lane has read the stage the next copy overwrites
-        if (tile + NS * step < tiles && limit) fetch(tile + NS * step, stage);
+        if (tile + NS * step < tiles) fetch(tile + NS * step, stage);
         advance();
     }
-    // what was asked for beyond the kept rows lands too, before its place is used again
+    // What was asked for and not used, beyond the kept rows or after a wait that gave up, lands too, before its place is used
+    // again or the CTA ends.
 #pragma unroll 1
-    for (; tile < all_tiles && tile < first_tile + NS * step; tile += step) {
-        landed();
-        advance();
-    }
+    for (int k = 0; k < NS; ++k, tile += step)
+        if (tile < all_tiles && (tile < first_tile + NS * step || tile < tiles)) {
+            landed(lost ? tc::kWaitCycles : p.wait_cycles);
+            advance();
+        }
 
     // ---- the warp's rows
 #pragma unroll

@@ -26,6 +26,7 @@ decltype(&shotkv_decode_step) g_decode_step;
 decltype(&shotkv_decode_step_attend) g_decode_step_attend;
 decltype(&shotkv_norm_rope) g_norm_rope;
 decltype(&shotkv_compact_kv4) g_compact_kv4;
+decltype(&shotkv_unpack_kv4) g_unpack_kv4;
 decltype(&shotkv_decode_step_kv4) g_decode_step_kv4;
 decltype(&shotkv_decode_step_attend_kv4) g_decode_step_attend_kv4;
 
@@ -297,6 +298,18 @@ PyObject* compact_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return [=] { return g_compact_kv4(c, d, K, V, idx, count, mcap, K4, V4, st); };
     });
 }
+PyObject* unpack_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(a, n, [](Args& g) {
+        auto* c = g.context();
+        auto* d = g.structure<shotkv_dims>(g_dims);
+        auto *K4 = g.u8(), *V4 = g.u8();
+        auto* count = g.i32();
+        const int32_t mcap = (int32_t)g.integer(INT32_MIN, INT32_MAX);
+        auto *Kc = g.bf16(), *Vc = g.bf16();
+        void* st = g.stream();
+        return [=] { return g_unpack_kv4(c, d, K4, V4, count, mcap, Kc, Vc, st); };
+    });
+}
 PyObject* decode_step_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(a, n, [](Args& g) {
         auto* c = g.context();
@@ -321,13 +334,13 @@ PyObject* decode_step_attend_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// init(Dims, Policy, DecodeState, Rope, addresses of the ten functions in the order above)
+// init(Dims, Policy, DecodeState, Rope, addresses of the eleven functions in the order above)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    constexpr int kTypes = 4, kFunctions = 10;
+    constexpr int kTypes = 4, kFunctions = 11;
     bool ok = n == kTypes + kFunctions;
     for (int k = 0; ok && k < kTypes; ++k) ok = PyType_Check(a[k]);
     if (!ok) {
-        PyErr_SetString(PyExc_TypeError, "init(Dims, Policy, DecodeState, Rope, ten addresses)");
+        PyErr_SetString(PyExc_TypeError, "init(Dims, Policy, DecodeState, Rope, eleven addresses)");
         return nullptr;
     }
     void* f[kFunctions];
@@ -349,14 +362,15 @@ PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
     g_decode_step_attend = reinterpret_cast<decltype(g_decode_step_attend)>(f[5]);
     g_norm_rope = reinterpret_cast<decltype(g_norm_rope)>(f[6]);
     g_compact_kv4 = reinterpret_cast<decltype(g_compact_kv4)>(f[7]);
-    g_decode_step_kv4 = reinterpret_cast<decltype(g_decode_step_kv4)>(f[8]);
-    g_decode_step_attend_kv4 = reinterpret_cast<decltype(g_decode_step_attend_kv4)>(f[9]);
+    g_unpack_kv4 = reinterpret_cast<decltype(g_unpack_kv4)>(f[8]);
+    g_decode_step_kv4 = reinterpret_cast<decltype(g_decode_step_kv4)>(f[9]);
+    g_decode_step_attend_kv4 = reinterpret_cast<decltype(g_decode_step_attend_kv4)>(f[10]);
     Py_RETURN_NONE;
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {FAST(init), FAST(prefill_score), FAST(select_shots), FAST(compact_kv), FAST(prefill_compress),
-                           FAST(decode_step), FAST(decode_step_attend), FAST(norm_rope), FAST(compact_kv4),
+                           FAST(decode_step), FAST(decode_step_attend), FAST(norm_rope), FAST(compact_kv4), FAST(unpack_kv4),
                            FAST(decode_step_kv4), FAST(decode_step_attend_kv4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, g_methods};
 

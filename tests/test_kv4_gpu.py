@@ -469,6 +469,27 @@ def test_steps_on_streams_of_their_own(ctx):
         s.check(True, [(0, 0), (1, 1), (2, 1)])
 
 
+@pytest.mark.parametrize("shape", [(1, 1, 1, 4, 128, 4000, 20), (30, 8, 8, 4, 128, 2000, 20)])
+def test_a_wait_that_gives_up_leaves_the_context_usable(ctx, shape):
+    """With a limit of one cycle the waits for tiles (and for a cluster's messages) may give up: the step ends, the next call says so
+    once, and a new state steps as ever."""
+    s = Step(ctx, *shape)
+    torch.cuda.synchronize()
+    skv.shotkv_set_wait_limit(ctx, 1)
+    try:
+        s.run(True)
+        torch.cuda.synchronize()
+    finally:
+        skv.shotkv_set_wait_limit(ctx, 0)
+    try:
+        t = Step(ctx, *shape)                                # its packing is a call, too
+    except skv.ShotKVError as e:
+        assert e.code == skv.ERR_TIMEOUT
+        t = Step(ctx, *shape)
+    t.run(True)
+    t.check(True, [(0, 0), (shape[0] - 1, shape[1] - 1)])
+
+
 def test_results_do_not_change_from_call_to_call(ctx):
     for shape in ((1, 1, 8, 4, 128, 1500, 100), (8, 8, 8, 4, 64, 200, 30)):
         outs = []
