@@ -41,6 +41,11 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
                  : "memory");
 }
 
+__device__ __forceinline__ uint64_t sub_pairs(uint64_t a, uint64_t b) {
+    uint64_t d;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 // Operand columns 0 .. 3 are one number of every key, columns 4 .. 7 another, and the lanes of columns 0 .. 3 have both of keys 0 .. 7, those of
 // columns 4 .. 7 (`second`) of keys 8 .. 15: what each contributes to the two 8 x 8 matrices.
 __device__ __forceinline__ void halves_of_columns(uint32_t one, uint32_t another, bool second, uint32_t& keys0, uint32_t& keys8) {
@@ -91,13 +96,13 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 // products are summed for themselves and then added (one sum for all of a warp's 26 tiles: outputs 4.2e-6 off in the
 // 2-norm, so 0.00e-7).
 template <int D, bool ATTEND, bool FUSED, bool PAIRED>
-__global__ void __launch_bounds__(StepKv4<D, ATTEND>::kWarps * 32, FUSED ? 3 : ATTEND ? 4 : 5)
+__global__ void __launch_bounds__(StepKv4<D, ATTEND>::kWarps * 32, FUSED ? 3 : ATTEND ? 4 : 6)
 decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const PackedCache cache) {
     using Cfg = StepKv4<D, ATTEND>;
     using F = Kv4<D>;
     constexpr int NB = D / 32, NC = D / 64, VPR = D / 8, MT = D / 16;
     constexpr int NW = Cfg::kWarps, NS = Cfg::kStages;
-    constexpr float kLift = 10.f, kHighest = 13.f, kUnset = -1e30f;
+    constexpr float kLift = 10.f, kHighest = 8192.f, kUnset = -1e30f;
     extern __shared__ __align__(128) unsigned char dsm[];
     unsigned char* ring = dsm;                               // [NW][NS][keys | values]; later each warp's outputs
     uint4* sq = reinterpret_cast<uint4*>(ring + Cfg::kRingBytes + Cfg::kBarBytes);   // [NB][32 lanes] the queries as B fragments, f16
@@ -108,7 +113,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     float4* sin = reinterpret_cast<float4*>(stab + p.nsplit * 8);
     unsigned long long* arrived = reinterpret_cast<unsigned long long*>(sred) - 1;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;     // (so that the warp's are uniform)
     const int g = lane >> 2, t4 = lane & 3;
     const int u = blockIdx.x / p.nsplit, rank = blockIdx.x - u * p.nsplit;
     const QuadShare qs = quads_of<D>(p.G, p.nsplit, rank);
@@ -272,14 +277,17 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             x[i] = j < n ? (second ? c[2 + (i & 1)] : c[i]) * p.scale_log2 : SHOTKV_NEG_INF;
             if (j < n && r < p.G) sdec[r * p.Dcap + j] = x[i];
         }
-        const float high[2] = {fmaxf(x[0], x[2 * KL - 2]), fmaxf(x[1], x[2 * KL - 1])};
-        if (__any_sync(0xffffffffu, high[0] > ref[0] + kHighest || high[1] > ref[1] + kHighest)) raise(high);
-        float w[2 * KL];
+        float w[2 * KL], most = 0.f;
 #pragma unroll
-        for (int i = 0; i < 2 * KL; ++i) {
-            w[i] = ex2f(x[i] - ref[i & 1]);
-            z[i & 1] += w[i];
+        for (int i = 0; i < 2 * KL; ++i) most = fmaxf(most, w[i] = ex2f(x[i] - ref[i & 1]));
+        if (__any_sync(0xffffffffu, most > kHighest)) {
+            const float high[2] = {fmaxf(x[0], x[2 * KL - 2]), fmaxf(x[1], x[2 * KL - 1])};
+            raise(high);
+#pragma unroll
+            for (int i = 0; i < 2 * KL; ++i) w[i] = ex2f(x[i] - ref[i & 1]);
         }
+#pragma unroll
+        for (int i = 0; i < 2 * KL; ++i) z[i & 1] += w[i];
         if (ATTEND) {
             // weights as B fragments in three bf16 parts (2^-24), keys in their order on the product's inner side; paired, the
             // first two are the columns of one fragment
@@ -324,15 +332,22 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 
     // ---- packed rows
     const int M = min(kept, p.Mcap), tiles = kv4_tiles(M);
-    // what is left of the factors of codes_subnormal for this lane's keys: c + 8 is multiplied, and of key g + 8 sixteen times that
-    float ease[KL], z_by[KL], z_less[KL];
+    // what codes_subnormal leaves for this lane's keys: c + 8 is multiplied, and of key g + 8 sixteen times that
+    float scales[KL][2], z_by[KL], z_less[KL];
 #pragma unroll
     for (int k = 0; k < KL; ++k) {
         const bool high = k || second;
-        ease[k] = high ? 0.0625f : 1.f, z_by[k] = high ? 16.f : 1.f, z_less[k] = high ? -128.f : -8.f;
+        z_by[k] = high ? 16.f : 1.f, z_less[k] = high ? -128.f : -8.f;
+        scales[k][0] = scale2[0] * (high ? 0.0625f : 1.f), scales[k][1] = scale2[1] * (high ? 0.0625f : 1.f);
     }
-    float unit = 1.f;                                        // O and wz are in units of 1 / unit
-    bool begun = false;
+    float unit = 1.f;                                        // O and wz are in units of 1 / unit, of odd dimensions O in a sixteenth of it
+    if (ATTEND)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) O[mt][2] *= 16.f, O[mt][3] *= 16.f;
+    // in registers that the compiler cannot make anew for each use
+    Under under = codes_under();
+    under.k1024 |= (uint32_t)p.nsplit >> 31, under.k1032 |= (uint32_t)p.nsplit >> 31;
+    float guard = 0x1p110f;                                  // `unit` once it is set, until then a number that sets it
     int stage = 0;
     uint32_t parity = 0;
     // The same answer in all lanes; `limit` cycles at most.
@@ -353,7 +368,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         lost = !landed(p.wait_cycles);
         if (lost) break;
         const unsigned char* st = mine + stage * Cfg::kStageBytes;
-        // of the tile's halves hb: this lane's keys' two rows (still with `ease` to come), and words of the values
+        // of the tile's halves hb: this lane's keys' two rows (still to be scaled), and words of the values
         float x[2][2 * KL] = {};
         uint32_t vw[2][KL];
 #pragma unroll
@@ -402,27 +417,39 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 #pragma unroll
                 for (int k = 0; k < KL; ++k)
                     if (tile * 32 + hb * 16 + key_of(k) >= M) x[hb][2 * k] = x[hb][2 * k + 1] = SHOTKV_NEG_INF, vw[hb][k] = 0;
-        bool out = false;
-        {
-            float high[2];
+        // weights relative to the references, which are set again where one is out of range
+        float w[2][2 * KL];
+        const auto weigh = [&] {
+            const uint64_t down = tc::pack2(-ref[0], -ref[1]);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                high[r] = fmaxf(x[0][r], x[1][r]) * ease[0];
-                if (KL == 2) high[r] = fmaxf(high[r], fmaxf(x[0][2 * KL - 2 + r], x[1][2 * KL - 2 + r]) * ease[KL - 1]);
-                high[r] *= scale2[r];
-            }
-            out = high[0] > ref[0] + kHighest || high[1] > ref[1] + kHighest;
-            if (ATTEND) {
-                float s = fmaxf(bf16_high(vw[0][0]), bf16_high(vw[1][0]));
-                if (KL == 2) s = fmaxf(s, fmaxf(bf16_high(vw[0][KL - 1]), bf16_high(vw[1][KL - 1])));
-                out |= !begun || s * unit >= 4.f;
-                if (__any_sync(0xffffffffu, out)) {
-                    raise(high);
+            for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                for (int k = 0; k < 2 * KL; k += 2) {
+                    tc::unpack2(tc::ffma2(tc::pack2(x[hb][k], x[hb][k + 1]), tc::pack2(scales[k / 2][0], scales[k / 2][1]), down), w[hb][k], w[hb][k + 1]);
+                    w[hb][k] = ex2f(w[hb][k]), w[hb][k + 1] = ex2f(w[hb][k + 1]);
+                }
+        };
+        weigh();
+        {
+            float most = 0.f, s = 0.f;
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                for (int k = 0; k < KL; ++k) {
+                    most = fmaxf(most, fmaxf(w[hb][2 * k], w[hb][2 * k + 1]));
+                    if (ATTEND) s = fmaxf(s, bf16_high(vw[hb][k]));
+                }
+            if (__any_sync(0xffffffffu, most > kHighest || (ATTEND && s * guard >= 4.f))) {
+                float high[2] = {SHOTKV_NEG_INF, SHOTKV_NEG_INF};
+#pragma unroll
+                for (int i = 0; i < 4 * KL; ++i) high[i & 1] = fmaxf(high[i & 1], x[i / (2 * KL)][i % (2 * KL)] * scales[i % (2 * KL) / 2][i & 1]);
+                raise(high);
+                if (ATTEND) {
 #pragma unroll
                     for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
                     const int e = min(max((int)(__float_as_uint(s) >> 23), 67), 250);      // its exponent
                     float next = __uint_as_float((uint32_t)(254 - e) << 23);
-                    if (begun) next = fminf(unit, next);
+                    if (guard == unit) next = fminf(unit, next);
                     const float al = next / unit;
 #pragma unroll
                     for (int r = 0; r < 2; ++r) wz[r] *= al;
@@ -430,36 +457,30 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
                         for (int c = 0; c < 4; ++c) O[mt][c] *= al;
-                    unit = next;
-                    begun = true;
+                    unit = guard = next;
                 }
-            } else if (__any_sync(0xffffffffu, out)) {
-                raise(high);
+                weigh();
             }
         }
-        // weights, and with them (ATTEND) the values' scales as B fragments: high parts and remainders
+        // their sums, and with the values' scales (ATTEND) they are B fragments: high parts and remainders
         uint32_t wh[2][2], wl[2][2];
-        const uint64_t down = tc::pack2(-ref[0], -ref[1]);
         uint64_t zz = tc::pack2(z[0], z[1]);
 #pragma unroll
         for (int hb = 0; hb < 2; ++hb) {
             uint32_t hi[KL], lo[KL];
 #pragma unroll
             for (int k = 0; k < KL; ++k) {
-                float w[2];
-                const uint64_t scales = tc::pack2(scale2[0] * ease[k], scale2[1] * ease[k]);
-                tc::unpack2(tc::ffma2(tc::pack2(x[hb][2 * k], x[hb][2 * k + 1]), scales, down), w[0], w[1]);
-                w[0] = ex2f(w[0]), w[1] = ex2f(w[1]);
-                zz = tc::fadd2(zz, tc::pack2(w[0], w[1]));
+                float w0 = w[hb][2 * k], w1 = w[hb][2 * k + 1];
+                zz = tc::fadd2(zz, tc::pack2(w0, w1));
                 if (ATTEND) {
                     const float s = bf16_high(vw[hb][k]) * unit, zs = bf16_low(vw[hb][k]);
-                    w[0] *= s, w[1] *= s;
-                    wz[0] = fmaf(w[0], zs, wz[0]);
-                    wz[1] = fmaf(w[1], zs, wz[1]);
-                    hi[k] = pack_f16(w[0], w[1]);
+                    w0 *= s, w1 *= s;
+                    wz[0] = fmaf(w0, zs, wz[0]);
+                    wz[1] = fmaf(w1, zs, wz[1]);
+                    hi[k] = pack_f16(w0, w1);
                     const float2 f = unpack_f16(hi[k]);
                     float rest[2];
-                    tc::unpack2(tc::ffma2(tc::pack2(f.x, f.y), tc::pack2(-1.f, -1.f), tc::pack2(w[0], w[1])), rest[0], rest[1]);
+                    tc::unpack2(sub_pairs(tc::pack2(w0, w1), tc::pack2(f.x, f.y)), rest[0], rest[1]);
                     lo[k] = pack_f16(rest[0], rest[1]);
                 }
             }
@@ -482,10 +503,10 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                 for (int i = 0; i < 4; ++i) {
                     float c[4];
                     uint32_t a[4];
-                    codes_f16(e0[i], a);
+                    codes_f16(e0[i], under, a);
                     if (PAIRED) mma_f16_16816_first(c, a, wh[0][0], wh[0][1]);
                     else mma_f16_16816_first(c, a, wl[0][0], wl[0][1]), mma_f16_16816(c, a, wh[0][0], wh[0][1]);
-                    codes_f16(e1[i], a);
+                    codes_f16(e1[i], under, a);
                     if (!PAIRED) mma_f16_16816(c, a, wl[1][0], wl[1][1]);
                     mma_f16_16816(c, a, wh[1][0], wh[1][1]);
                     float(&o)[4] = O[h * 4 + i];
@@ -535,7 +556,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     for (int e = 0; e < 2; ++e) {
                         float x = O[h * 4 + i][2 * e + r];
                         if (PAIRED) x += __shfl_xor_sync(0xffffffffu, x, 2);
-                        v[2 * i + e] = (x + wz[r]) * back;
+                        v[2 * i + e] = (e ? fmaf(x, 0.0625f, wz[r]) : x + wz[r]) * back;
                     }
                 if (!second) {
                     *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);

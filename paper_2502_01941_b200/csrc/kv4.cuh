@@ -202,28 +202,32 @@ __global__ void __launch_bounds__(kPackThreads) compact_kv4_kernel(const uint4* 
 }
 
 // ---- codes into numbers ------------------------------------------------------------------------
-// (w & MASK) | UNDER as the one instruction it is (written out, its two constants made two of it: 289 of them a tile
-// of the decode step instead of 170).
-template <uint32_t MASK, uint32_t UNDER>
-__device__ __forceinline__ uint32_t and_or(uint32_t w) {
+// (w & MASK) | under as the one instruction it is (written out, its two constants made two of it).
+template <uint32_t MASK>
+__device__ __forceinline__ uint32_t and_or(uint32_t w, uint32_t under) {
     uint32_t d;
-    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "n"(MASK), "n"(UNDER));
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(d) : "r"(w), "n"(MASK), "r"(under));
     return d;
 }
-// A word's four registers of an A fragment: pairs of codes -8..7 as f16, exact.  A byte under the significand of 1024
-// is 1024 + n + 16 n', its upper nibble under that of 1032 is 1032 + 16 n': their difference is n - 8, and a sixteenth of
-// the second, less 72.5, n' - 8.  (Eight instructions a word, four of them on the pipe of the logical operations; each nibble by itself
-// under 1024 takes nine and five.)
-__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t (&a)[4]) {
+// What codes are put under: 1024 and 1032, as pairs of f16.
+struct Under {
+    uint32_t k1024, k1032;
+};
+__device__ __forceinline__ Under codes_under() { return Under{0x64006400u, 0x64086408u}; }
+// A word's four registers of an A fragment: pairs of codes -8..7 as f16, of registers 1 and 3 sixteen times as much, exact.
+// A byte under the significand of 1024 is 1024 + n + 16 n', its upper nibble under that of 1032 is 1032 + 16 n': their
+// difference is n - 8, and the second less 1160 is 16 (n' - 8).  (Eight instructions a word, four of them on the pipe of the logical
+// operations; each nibble by itself under 1024 takes nine and five.)
+__device__ __forceinline__ void codes_f16(uint32_t w, const Under& k, uint32_t (&a)[4]) {
     const auto h = [](uint32_t x) { return *reinterpret_cast<const __half2*>(&x); };
     const auto u = [](__half2 x) { return *reinterpret_cast<const uint32_t*>(&x); };
-    const __half2 sixteenth = h(0x2c002c00u), less = h(0xd488d488u);      // 1/16, -72.5
-    const uint32_t low = and_or<0x00ff00ffu, 0x64006400u>(w), high = __byte_perm(w, 0x64646464u, 0x4341);
-    const uint32_t low1 = and_or<0x00f000f0u, 0x64086408u>(w), high1 = and_or<0x00f000f0u, 0x64086408u>(high);
+    const __half2 less = h(0xe488e488u);                                  // -1160
+    const uint32_t low = and_or<0x00ff00ffu>(w, k.k1024), high = __byte_perm(w, k.k1024, 0x5351);
+    const uint32_t low1 = and_or<0x00f000f0u>(w, k.k1032), high1 = and_or<0x00f000f0u>(high, k.k1032);
     a[0] = u(__hsub2(h(low), h(low1)));
-    a[1] = u(__hfma2(h(low1), sixteenth, less));
+    a[1] = u(__hadd2(h(low1), less));
     a[2] = u(__hsub2(h(high), h(high1)));
-    a[3] = u(__hfma2(h(high1), sixteenth, less));
+    a[3] = u(__hadd2(h(high1), less));
 }
 // The same as f16 subnormals: code + 8 in units of 2^-24, of registers 1 and 3 (rows g + 8 of a product) of 2^-20.
 __device__ __forceinline__ void codes_subnormal(uint32_t w, uint32_t (&a)[4]) {
@@ -260,6 +264,7 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kv4_kernel(const unsigned
 #pragma unroll
     for (int i = 0; i < 4; ++i) vm[i] = Vm[2 * t + (i & 1) + 8 * (i >> 1)];
     const auto value = [](float c, uint32_t m) { return bf16_high(m) * (c + bf16_low(m)); };
+    const Under under = codes_under();
     const auto pair = [](float a, float b) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&v);
@@ -274,10 +279,11 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kv4_kernel(const unsigned
         for (int h = 0; h < 2; ++h) {
             const uint4 w4 = kw[kb / 2];
             uint32_t a[4];
-            codes_f16(kb & 1 ? (h ? w4.w : w4.z) : (h ? w4.y : w4.x), a);
+            codes_f16(kb & 1 ? (h ? w4.w : w4.z) : (h ? w4.y : w4.x), under, a);
 #pragma unroll
             for (int p = 0; p < 4; ++p) {
-                const float2 c = split(a[p]);
+                float2 c = split(a[p]);
+                if (p & 1) c.x *= 0.0625f, c.y *= 0.0625f;
                 const uint32_t m = km[(p & 1) * NB + kb];
                 r[p & 1][2 * h + (p >> 1)] = pair(value(c.x, m), value(c.y, m));
             }
@@ -292,12 +298,12 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kv4_kernel(const unsigned
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             uint32_t a[4];
-            codes_f16(w4[i], a);
+            codes_f16(w4[i], under, a);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {                  // rows 2 t + 8 h and the next
                 const float2 even = split(a[2 * h]), odd = split(a[2 * h + 1]);
-                r[2 * h][i] = pair(value(even.x, vm[2 * h]), value(odd.x, vm[2 * h]));
-                r[2 * h + 1][i] = pair(value(even.y, vm[2 * h + 1]), value(odd.y, vm[2 * h + 1]));
+                r[2 * h][i] = pair(value(even.x, vm[2 * h]), value(odd.x * 0.0625f, vm[2 * h]));
+                r[2 * h + 1][i] = pair(value(even.y, vm[2 * h + 1]), value(odd.y * 0.0625f, vm[2 * h + 1]));
             }
         }
 #pragma unroll
