@@ -1541,7 +1541,7 @@ namespace {
 // 2, 185 keys 8.5 -> 7.1; 1 block: 8 heads of 1,150 keys 7.0 -> 7.3).  Scores alone take less per block than a larger
 // cluster costs (8 heads of 3,400 keys 5.3 us with 2.5 blocks, 6.1 with 2, 5.7 with 3; with 2.5, 1 to 148 units of 64
 // to 8,192 keys all take what they took with 2 and at most eight CTAs, within 2 %, or less).
-constexpr int kLeastAttend = 8, kLeastScore = 15, kLeastKv4 = 8;
+constexpr int kLeastAttend = 8, kLeastScore = 15;
 template <class Smem>
 int decode_split(const DecodeRoom& room, Smem&& smem, long long U, long long keys, int warps, int least) {
     int n = kMaxSplit;
@@ -1624,14 +1624,21 @@ int launch_decode_score(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishPara
     return launch(ctx, kernel, grid, 256, whole, stream, 1, kEarly, p, f);
 }
 
-// The same over a prompt in 4 bits.
+// The same over a prompt in 4 bits.  A unit is shared by as many CTAs as above, but by no more than make two to an SM (one and a
+// half in clusters of more than eight, which fit fewer places), unless every CTA keeps a long share: more of them cost
+// more at the end than they gain.  As many as run | this rule, with the attention output and 131 entries: 64 units of
+// 3,276 rows 16.8 | 14.5 us a step, of 8,000 27.2 | 24.1, 32 of 3,276 10.9 | 9.8, 128 of 3,276 23.9 | 22.5, 256 of 333 14.4 | 12.6;
+// a long share: 256 of 8,000 rows with two CTAs each 66.3, with one 70.7.
+constexpr int kLeastKv4 = 8, kLongShareKv4 = 3200;      // of a block of 16 rows a warp, in sixths; rows a CTA
 template <int D, bool ATTEND, bool PAIRED>
 int launch_decode_kv4_t(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
                         cudaStream_t stream) {
     constexpr int threads = StepKv4<D, ATTEND>::kWarps * 32;
     const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND][PAIRED];
     const auto smem_of = [&](int n) { return kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, n); };
-    p.nsplit = decode_split(room[0], smem_of, U, (long long)p.Mcap + p.n_old + 1, StepKv4<D, ATTEND>::kWarps, kLeastKv4);
+    const long long keys = (long long)p.Mcap + p.n_old + 1;
+    p.nsplit = decode_split(room[0], smem_of, U, keys, StepKv4<D, ATTEND>::kWarps, kLeastKv4);
+    while (p.nsplit > 1 && 2 * U * p.nsplit > (p.nsplit > 8 ? 3 : 4) * ctx->sm_count && keys < (long long)kLongShareKv4 * p.nsplit) --p.nsplit;
     const size_t smem = smem_of(p.nsplit), end = fused_end_smem_bytes(p.Hkv, f.n, f.k < f.n);
     const dim3 grid(U * p.nsplit);
     ended = smem + end <= kBigSmem &&
