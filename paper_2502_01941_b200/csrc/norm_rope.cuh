@@ -30,14 +30,14 @@ struct NormRopeParams {
 // (cos, sin) are read once for all of its heads and multiplied by the weights then, so that an element takes two products
 // of two numbers each, and one by 1 / sqrt.  The other element of a pair comes as it lies in memory: of halves from the lane
 // rot / 16 away, of neighbours from the same word.
-constexpr int kRopeThreads = 256, kRopeAhead = 4;
+constexpr int kRopeThreads = 128, kRopeAhead = 4;
 template <int D>
 __host__ __device__ constexpr int rope_heads_a_piece() { return 32 / (D / 8); }
-// Pieces a lane for a row of `heads`, a power of two of at most `ahead`, and the sections of it.
+// Pieces a lane for a row of `heads`, a power of two of at most `most`, and the sections of it.
 template <int D>
-inline void rope_share(int heads, int ahead, int& vectors, int& sections) {
+inline void rope_share(int heads, int most, int& vectors, int& sections) {
     const int all = (heads + rope_heads_a_piece<D>() - 1) / rope_heads_a_piece<D>();
-    for (vectors = 1; vectors < all && vectors < ahead;) vectors *= 2;
+    for (vectors = 1; vectors < all && vectors < most;) vectors *= 2;
     sections = (all + vectors - 1) / vectors;
 }
 
@@ -211,7 +211,7 @@ __device__ __forceinline__ void rope_queries(const NormRopeParams& p, int index)
     }
 }
 template <int D>
-__global__ void __launch_bounds__(kRopeThreads, 3) norm_rope_kernel(const NormRopeParams p) {
+__global__ void __launch_bounds__(kRopeThreads, 6) norm_rope_kernel(const NormRopeParams p) {
     constexpr int NW = kRopeThreads / 32;
     const int warp = threadIdx.x >> 5, x = blockIdx.x;
     grid_release();

@@ -1234,11 +1234,14 @@ int shotkv_norm_rope(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_rope
     // of the queries all rows, or those in the window
     const int to_window = dims->N - dims->W - rope->first;
     p.q_first = q_out || to_window < 0 ? 0 : std::min(to_window, (int)rope->rows);
+    // a warp's pieces are `ahead`; where there is little to do, fewer of them are used and more warps
     const auto ctas = [&](int heads, int rows, int ahead, int& vectors, int& sections) -> long long {
-        if (dims->d == 128) rope_share<128>(heads, ahead, vectors, sections);
-        else rope_share<64>(heads, ahead, vectors, sections);
-        const long long warps = (long long)((rows + ahead / vectors - 1) / (ahead / vectors)) * sections;
-        return (warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+        for (int most = ahead;; most /= 2) {
+            if (dims->d == 128) rope_share<128>(heads, most, vectors, sections);
+            else rope_share<64>(heads, most, vectors, sections);
+            const long long warps = (long long)((rows + ahead / vectors - 1) / (ahead / vectors)) * sections;
+            if (most <= 2 || warps * dims->B >= 4LL * ctx->sm_count) return (warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
+        }
     };
     const long long kv = ctas(dims->Hkv, rope->rows, kRopeAhead, p.kv_vectors, p.kv_sections);
     const long long grid = kv + ctas(dims->H, rope->rows - p.q_first, 2 * kRopeAhead, p.q_vectors, p.q_sections);
