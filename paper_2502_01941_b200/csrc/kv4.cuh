@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t codes_word(const float (&lo)[4], const float
 // sixteen 16-byte loads a lane in flight, and what it loads are the very elements of its own code words, so that nothing
 // goes through shared memory.  The lanes that hold a group's elements fold their extremes together and each works out
 // the grid of other groups.  grid = (warps' halves of a unit, Hkv, B*L).
-constexpr int kPackThreads = 256;
+constexpr int kPackThreads = 128;
 template <int D>
 __global__ void __launch_bounds__(kPackThreads) compact_kv4_kernel(const uint4* K, const uint4* V, const int* kept_idx, const int* kept_count,
                                                                   int Hkv, int N, int Mcap, unsigned char* K4, unsigned char* V4) {

@@ -370,10 +370,10 @@ def test_caches_beyond_four_gigabytes(ctx, attend):
     s.check(attend, [(0, 0), (B - 1, L - 1), (B - 1, L - 2)])
 
 
-def test_many_steps_with_evictions_are_the_bf16_steps(ctx):
+@pytest.mark.parametrize("B,L,Hkv,G,d,M,steps", [(2, 2, 2, 4, 128, 150, 70), (12, 3, 8, 5, 64, 90, 22), (1, 1, 8, 8, 128, 700, 15)])
+def test_many_steps_with_evictions_are_the_bf16_steps(ctx, B, L, Hkv, G, d, M, steps):
     """Rows that 4 bits and bf16 both hold as they are: the two forms of the prompt take a generation through the same states.
     The prompt's form changes in mid-generation for a third state."""
-    B, L, Hkv, G, d, M, steps = 2, 2, 2, 4, 128, 150, 70
     g = torch.Generator(device="cuda").manual_seed(4)
     K, V = (torch.randint(-8, 8, (B, L, Hkv, M, d), generator=g, device="cuda").float() for _ in range(2))
     for t in (K, V):                                         # every group reaches over the whole grid, of a scale of 1/8
@@ -451,6 +451,31 @@ def test_a_captured_step_replays(ctx, B, Hkv, M, n_old, attend):
         graph.replay()
         torch.cuda.synchronize()
         s.check(attend, [(0, 0), (B - 1, 0), (B // 2, 0)])
+
+
+def test_first_calls_may_be_captured():
+    """A process whose first calls of all are captured ones."""
+    import subprocess
+    import sys
+    code = (
+        "import sys; sys.path[:0] = ['tests', '.']\n"
+        "import numpy as np, torch, paper_2502_01941_b200 as skv, test_kv4_gpu as T, test_norm_rope_gpu as N\n"
+        "ctx = skv.Context(0)\n"
+        "pack, T.packed = T.packed, lambda ctx, dims, K, V, idx, counts, M: skv.alloc_kv4(dims, M)\n"
+        "s, r = T.Step(ctx, 2, 1, 2, 4, 64, 90, 10), N.Layer(2, 1, 4, 2, 64, 30, 5, 0, 30, 64)\n"
+        "Kc, Vc = torch.zeros_like(s.K), torch.zeros_like(s.V)\n"
+        "torch.cuda.synchronize()\n"
+        "g = torch.cuda.CUDAGraph()\n"
+        "with torch.cuda.graph(g):\n"
+        "    r.run(ctx)\n"
+        "    skv.shotkv_compact_kv4(ctx, s.dims, s.K, s.V, None, s.count, 90, s.K4, s.V4)\n"
+        "    skv.shotkv_unpack_kv4(ctx, s.dims, s.K4, s.V4, s.count, 90, Kc, Vc)\n"
+        "    s.run(True)\n"
+        "g.replay(); torch.cuda.synchronize()\n"
+        "s.check(True); r.check(); assert Kc.abs().sum() > 0\n"
+        "del g\n")
+    done = subprocess.run([sys.executable, "-c", code], cwd=__file__.rsplit("/tests/", 1)[0], capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, done.stderr[-2000:]
 
 
 def test_steps_on_streams_of_their_own(ctx):
