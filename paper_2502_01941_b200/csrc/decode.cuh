@@ -526,14 +526,14 @@ constexpr int kOutPitch = D + 4;                           // floats a row of a 
 // The end of a fused step in a CTA of NW warps, by all its threads after a barrier.  Shared memory: (m, z) of the warps' 8
 // rows in `sred`, the warps' outputs [8 rows][kOutPitch] in `sO`, `pitch` floats apart, logits of the decode entries in `sdec`;
 // of a cluster: `stab` [nsplit][8 rows] (m, z) of its CTAs, `sin` [nsplit][share + 1] their outputs, of which this CTA has
-// its share of the quads, and the barrier of what they send here.  `begin`: of a shared unit, the first decode entry among
-// this warp's blocks of 16.
+// its share of the quads, and the barrier of what they send here.  n decode entries follow M keys, and this warp's blocks of 16 keys
+// begin at `first` (the kernel that has the entries apart says M = 0).
 template <int D, int NW, bool FUSED>
 __device__ __forceinline__ void finish_attend(const DecodeParams& p, const DecodeFinishParams& f, const UnitPart& part, const QuadShare& qs,
                                               const FusedEnd& end, float2* sred, float* sdec, float2* stab, float4* sin,
-                                              unsigned long long* arrived, const float* sO, int pitch, int begin) {
+                                              unsigned long long* arrived, const float* sO, int pitch, int first, int M, int n) {
     constexpr int NT = NW * 32;
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, t4 = lane & 3, STRIDE = p.nsplit * NW * 16;
     const int quads = qs.quads, over = qs.over, share = qs.share, owned = qs.owned;
     float* out = p.out + ((size_t)part.bl * p.H + (size_t)part.hk * p.G) * D;
     if (p.nsplit > 1 && tid < 8 * p.nsplit) {                // every CTA's rows to every CTA
@@ -599,7 +599,8 @@ __device__ __forceinline__ void finish_attend(const DecodeParams& p, const Decod
     // at a time; whole units have them all here, and a lane each (768 units of 608 keys and 390 decode entries, d = 64: 46.3
     // -> 43.2 us a step, eight query heads to a KV head 50.8 -> 45.7)
     const bool whole = p.nsplit == 1;
-    entry_weights(sdec, p.Dcap, p.G, rm, riz, whole ? warp * 32 : begin, f.n, whole ? NT : p.nsplit * NW * 16, whole ? 32 : 16, [&](int j, float s) {
+    const int begin = whole ? warp * 32 : first + max(0, (M - 15 - first + STRIDE - 1) / STRIDE) * STRIDE - M;
+    entry_weights(sdec, p.Dcap, p.G, rm, riz, begin, n, whole ? NT : STRIDE, whole ? 32 : 16, [&](int j, float s) {
         if (FUSED) fused_send(end, f, part.hk, j, s, part.ctas);
         else p.partial[(size_t)part.u * p.Dcap + j] = s;
     });
@@ -882,8 +883,8 @@ __global__ void __launch_bounds__(AttendCfg<D>::kWarps * 32, 3) decode_attend_ke
         o[PITCH + 8] = O[mt][3];
     }
     __syncthreads();
-    finish_attend<D, NW, FUSED>(p, f, UnitPart{u, bl, hk, rank, first_cta, ctas}, qs, end, sred, sdec, stab, sin, arrived, sO, kWarpRing,
-                                first + max(0, (M - 15 - first + STRIDE - 1) / STRIDE) * STRIDE - M);
+    finish_attend<D, NW, FUSED>(p, f, UnitPart{u, bl, hk, rank, first_cta, ctas}, qs, end, sred, sdec, stab, sin, arrived, sO, kWarpRing, first,
+                                M, n);
 }
 
 }  // namespace shotkv

@@ -566,7 +566,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     }
     __syncthreads();
     if constexpr (ATTEND) {
-        finish_attend<D, NW, FUSED>(p, f, UnitPart{u, bl, hk, rank, first_cta, ctas}, qs, end, sred, sdec, stab, sin, arrived, sO, kPitch, turn * 16);
+        finish_attend<D, NW, FUSED>(p, f, UnitPart{u, bl, hk, rank, first_cta, ctas}, qs, end, sred, sdec, stab, sin, arrived, sO, kPitch,
+                                        turn * 16, 0, n);
     } else {
         bool ok = true;
         if (p.nsplit > 1) {
