@@ -46,32 +46,36 @@ __device__ __forceinline__ uint64_t sub_pairs(uint64_t a, uint64_t b) {
     asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
 }
-// Operand columns 0 .. 3 are one number of every key, columns 4 .. 7 another, and the lanes of columns 0 .. 3 have both of keys 0 .. 7, those of
-// columns 4 .. 7 (`second`) of keys 8 .. 15: what each contributes to the two 8 x 8 matrices.
-__device__ __forceinline__ void halves_of_columns(uint32_t one, uint32_t another, bool second, uint32_t& keys0, uint32_t& keys8) {
+// Of each of two matrices of 8 keys, columns 0 .. 3 are to be one number of every key and columns 4 .. 7 another.  The lanes of columns
+// 0 .. 3 have both numbers of the first matrix's keys, those of columns 4 .. 7 (`second`) of the other's: what each contributes to them.
+__device__ __forceinline__ void halves_of_columns(uint32_t one, uint32_t another, bool second, uint32_t& matrix0, uint32_t& matrix1) {
     const uint32_t other = __shfl_xor_sync(0xffffffffu, second ? one : another, 2);
-    keys0 = second ? other : one;
-    keys8 = second ? another : other;
+    matrix0 = second ? other : one;
+    matrix1 = second ? another : other;
 }
 
 struct PackedCache {
     const unsigned char *K4, *V4;            // [U][tiles][Kv4 tile]
 };
 
-template <int D, bool ATTEND>
+template <int D, bool ATTEND, bool PAIRED>
 struct StepKv4 {
     static constexpr int kWarps = 4;
     static constexpr int kStages = ATTEND ? 2 : 3;         // tiles in a warp's ring
     static constexpr int kStageBytes = Kv4<D>::kKeyTile + (ATTEND ? Kv4<D>::kValueTile : 0);
     static constexpr int kRingBytes = kWarps * kStages * kStageBytes;
     static constexpr int kBarBytes = kWarps * kStages * 8;
-    static constexpr int kQueryBytes = 8 * D * 2 + (D / 32) * 8 * 4;    // fragments of 8 rows in f16, their groups' sums
+    // CTAs on an SM that the registers are meant for.  (8 sequences x 32 layers, us a step.  d = 128, attention output: 4 and 5 CTAs the
+    // same, 5 with spilled registers.  d = 64: 700 rows 4 | 5 CTAs 53.6 | 47.7, but eight query rows 133.5 | 135.2.  Scores,
+    // d = 128 5 | 6 99.8 | 101.1, of 4 sequences 59.5 | 57.2; d = 64 6 | 8 60.6 | 64.9.)
+    static constexpr int ctas(bool fused) { return fused ? 3 : !ATTEND ? 6 : D == 64 && PAIRED ? 5 : 4; }
+    static constexpr int kQueryBytes = (PAIRED ? 2 : 1) * 8 * D * 2 + (D / 32) * 8 * 4;    // operands of 8 columns in f16, the rows' groups' sums
     static_assert(!ATTEND || 8 * kOutPitch<D> * 4 <= kStages * kStageBytes, "a warp's outputs take the place of its ring");
 };
-template <int D, bool ATTEND>
+template <int D, bool ATTEND, bool PAIRED>
 __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit) {
     const size_t shares = nsplit > 1 ? (size_t)nsplit * (16 + (ATTEND ? (G * D / 4 / nsplit + 1) * 4 : 0)) : 0;
-    using Cfg = StepKv4<D, ATTEND>;
+    using Cfg = StepKv4<D, ATTEND, PAIRED>;
     return Cfg::kRingBytes + Cfg::kBarBytes + Cfg::kQueryBytes + 16 + ((size_t)Cfg::kWarps * 16 + ((size_t)G * Dcap + 3) / 4 * 4 + shares) * 4;
 }
 
@@ -80,33 +84,42 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 //
 // Both products have the keys, or the values' dimensions, on the 16-row side, so that a packed word is an operand's
 // fragment but for the conversion, and the group's (up to 8) query rows on the side of 8:
-//   S[16 keys x 8 rows] = codes . q, one chain of products for every group of 32 dimensions, in f16: codes are whole numbers, and
-//     a query row, bf16, is multiplied by the power of two that takes its largest element to [2^14, 2^15), which leaves elements
-//     down to 2^-31 of it exact.  A logit is sum over groups s (S + z sum of q's 32 elements).
-//   O^T[16 dims x 8 rows] += codes^T . w^T with w = p s_v, p = 2^(logit - reference): the accumulator of S, transposed 8 by 8, is
+//   S[16 keys x 8 rows] = (c + 8) . q, one chain of products for every group of 32 dimensions, in f16: codes are whole numbers (as
+//     f16 subnormals: nothing but masks and a shift), and a query row, bf16, is multiplied by the power of two that takes its
+//     largest element to [2^14, 2^15), which leaves elements down to 2^-31 of it exact.  A logit is the sum over groups of
+//     s (S + (z - 8) times the sum of q's 32 elements).
+//   O^T[16 dims x 8 rows] += c^T . w^T with w = p s_v, p = 2^(logit - reference): the accumulator of S, transposed 8 by 8, is
 //     the other operand, an f16 pair (high part and remainder: 2^-22 of w, or 2^-35 of the row's largest where that is more).  z
-//     is added once a row: sum of w z_v.  PAIRED, for groups of up to four rows: the remainders are columns 4 .. 7 of the one
-//     operand whose columns 0 .. 3 are the high parts, so that one product does for both.  (8 sequences x 32 layers, four rows:
-//     MMM us a step, MMM with a product for each part.)
+//     is added once a row: sum of w z_v.
+// PAIRED, for groups of up to four rows: the columns 4 .. 7 are the same rows again.  The remainders are in these columns of the one
+// operand whose columns 0 .. 3 are the high parts, so that one product does for both, and the lanes of columns 0 .. 3 have the
+// logits of one half of a tile, those of columns 4 .. 7 of the other.  (8 sequences x 32 layers, 3,276 rows, 145
+// entries, four query rows: 189 us a step, 217 without.)
 //
 // f16 ends at 65504, so both factors are kept in range by references that change seldom: a row's reference is 2^10 below its
 // maximum when it was last set and is set again by a tile whose p would exceed 2^13, and the values' scales are multiplied by a
 // power of two that takes the largest of the first tile to [1, 2) and is set again when one exceeds 4.  One vote a tile
 // decides that neither has happened.  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
-// products are summed for themselves and then added (one sum for all of a warp's 26 tiles: outputs 4.2e-6 off in the
-// 2-norm, so 0.00e-7).
+// products are summed for themselves and then added: one sum for all of a warp's 26 tiles left the outputs 4.2e-6 off in the
+// 2-norm, so they are 5.5e-7 off (elementary operations in 32 bits: 9.3e-7).
+//
+// What bounds it: bytes from HBM where calls are far apart (that step reads 1.09 GB: 178 us with kept counts that differ, 6.1 TB/s), and
+// the power cap where they follow one another for long (199 to 210 us from GPU to GPU, at 1.6 to 1.7 GHz): about 480 instructions a tile, half of them
+// conversions and the groups' scales, at 0.6 to 0.7 a cycle and scheduler.  So what was saved is instructions (780 at first): bulk
+// copies that one lane asks for, no accumulator set to zero, constants that stay in registers, sums of two rows at a time.  More
+// CTAs on an SM, or one tile's values computed beside the next one's keys, gained nothing.  Scores alone read half: 96 us, 6.0 TB/s.
 template <int D, bool ATTEND, bool FUSED, bool PAIRED>
-__global__ void __launch_bounds__(StepKv4<D, ATTEND>::kWarps * 32, FUSED ? 3 : ATTEND ? 4 : 6)
+__global__ void __launch_bounds__(StepKv4<D, ATTEND, PAIRED>::kWarps * 32, StepKv4<D, ATTEND, PAIRED>::ctas(FUSED))
 decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const PackedCache cache) {
-    using Cfg = StepKv4<D, ATTEND>;
+    using Cfg = StepKv4<D, ATTEND, PAIRED>;
     using F = Kv4<D>;
     constexpr int NB = D / 32, NC = D / 64, VPR = D / 8, MT = D / 16;
     constexpr int NW = Cfg::kWarps, NS = Cfg::kStages;
     constexpr float kLift = 10.f, kHighest = 8192.f, kUnset = -1e30f;
     extern __shared__ __align__(128) unsigned char dsm[];
     unsigned char* ring = dsm;                               // [NW][NS][keys | values]; later each warp's outputs
-    uint4* sq = reinterpret_cast<uint4*>(ring + Cfg::kRingBytes + Cfg::kBarBytes);   // [NB][32 lanes] the queries as B fragments, f16
-    float* sqsum = reinterpret_cast<float*>(sq + NB * 32);                   // [NB][8 rows] their groups' sums
+    uint4* sq = reinterpret_cast<uint4*>(ring + Cfg::kRingBytes + Cfg::kBarBytes);   // [1, PAIRED 2][NB][32 lanes] the queries as B fragments, f16
+    float* sqsum = reinterpret_cast<float*>(sq + (PAIRED ? 2 : 1) * NB * 32);                   // [NB][8 rows] their groups' sums
     float2* sred = reinterpret_cast<float2*>(ring + Cfg::kRingBytes + Cfg::kBarBytes + Cfg::kQueryBytes + 16);   // [NW warps][8 rows]  (m, z)
     float* sdec = reinterpret_cast<float*>(sred + NW * 8);   // [G][Dcap]  logits of the decode entries
     float2* stab = reinterpret_cast<float2*>(sdec + ((p.G * p.Dcap + 3) & ~3));
@@ -120,7 +133,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     const int bl = u / p.Hkv, hk = u - bl * p.Hkv;
     const int first_cta = FUSED ? hk * p.nsplit : 0, ctas = p.Hkv * p.nsplit;   // in the cluster: the unit's first; FUSED: all
     FusedEnd end{};
-    if (FUSED) end = fused_end_at(dsm + kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, p.nsplit), f);
+    if (FUSED) end = fused_end_at(dsm + kv4_smem_bytes<D, ATTEND, PAIRED>(p.G, p.Dcap, p.nsplit), f);
     unsigned long long* bars = reinterpret_cast<unsigned long long*>(ring + Cfg::kRingBytes) + warp * NS;   // this warp's stages'
     if (lane == 0) {
 #pragma unroll
@@ -146,8 +159,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     // an operand is g, and of an accumulator 2*t4 and 2*t4 + 1, which are rows r0 and r0 + 1.
     const int g_row = PAIRED ? g & 3 : g, r0 = PAIRED ? (2 * t4) & 3 : 2 * t4;
     const bool second = PAIRED && t4 >= 2;                   // the columns of the weights' remainders
-    // Of the 16 keys of an accumulator a lane has keys g and g + 8, and both in both columns of a row where there are two: it
-    // goes on with the first or the second of them then (with both in all lanes, a tenth more instructions).
+    // Of 16 decode entries in an accumulator a lane has g and g + 8, and both in both columns of a row where there are two: it
+    // goes on with the first or the second of them then.
     constexpr int KL = PAIRED ? 1 : 2;
     const auto key_of = [&](int k) { return g + (k || second ? 8 : 0); };
     const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bl * p.H + (size_t)hk * p.G + g_row) * D);
@@ -214,7 +227,10 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             s += __shfl_xor_sync(0xffffffffu, s, 1);
             s += __shfl_xor_sync(0xffffffffu, s, 2);
             if (warp == kb) {
-                sq[kb * 32 + lane] = make_uint4(e[0], e[1], e[2], e[3]);
+                // paired, an operand for each half of a tile: the rows in columns 0 .. 3, and in columns 4 .. 7, the others zeros
+                const uint4 q = make_uint4(e[0], e[1], e[2], e[3]), none = make_uint4(0, 0, 0, 0);
+                sq[kb * 32 + lane] = PAIRED && g >= 4 ? none : q;
+                if (PAIRED) sq[(NB + kb) * 32 + lane] = g >= 4 ? q : none;
                 if (t4 == 0) sqsum[kb * 8 + g] = s * 0x1p-24f;
             }
         }
@@ -332,14 +348,13 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 
     // ---- packed rows
     const int M = min(kept, p.Mcap), tiles = kv4_tiles(M);
-    // what codes_subnormal leaves for this lane's keys: c + 8 is multiplied, and of key g + 8 sixteen times that
-    float scales[KL][2], z_by[KL], z_less[KL];
-#pragma unroll
-    for (int k = 0; k < KL; ++k) {
-        const bool high = k || second;
-        z_by[k] = high ? 16.f : 1.f, z_less[k] = high ? -128.f : -8.f;
-        scales[k][0] = scale2[0] * (high ? 0.0625f : 1.f), scales[k][1] = scale2[1] * (high ? 0.0625f : 1.f);
-    }
+    // codes_subnormal has c + 8 multiplied, and of key g + 8 sixteen times that
+    const float scales[2][2] = {{scale2[0], scale2[1]}, {scale2[0] * 0.0625f, scale2[1] * 0.0625f}};
+    // Paired, the products of both halves of a tile add up in one accumulator, the first half's in columns 0 .. 3: a lane has keys g
+    // and g + 8 of one of them (all columns with both halves' keys, one of each two chosen: 212 us a step
+    // at the power cap where this takes 208).
+    constexpr int HALVES = PAIRED ? 1 : 2;                   // of a tile, that a lane has keys of
+    const auto half_of = [&](int h) { return PAIRED ? (int)second : h; };
     float unit = 1.f;                                        // O and wz are in units of 1 / unit, of odd dimensions O in a sixteenth of it
     if (ATTEND)
 #pragma unroll
@@ -368,81 +383,92 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         lost = !landed(p.wait_cycles);
         if (lost) break;
         const unsigned char* st = mine + stage * Cfg::kStageBytes;
-        // of the tile's halves hb: this lane's keys' two rows (still to be scaled), and words of the values
-        float x[2][2 * KL] = {};
-        uint32_t vw[2][KL];
+        // of this lane's halves, logits of keys g (x[.][0..1], still to be scaled) and g + 8 (x[.][2..3]), and the values' words
+        float x[HALVES][4] = {};
+        uint32_t m[HALVES][2][NB], vw[HALVES][2];
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
-            const uint4* kc = reinterpret_cast<const uint4*>(st + hb * F::kHalfBytes) + lane;
-            uint32_t m[KL][NB];
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-            for (int k = 0; k < KL; ++k) {
-                const uint32_t* km = reinterpret_cast<const uint32_t*>(st + F::kCodeBytes) + (hb * 16 + key_of(k)) * NB;
+            for (int k = 0; k < 2; ++k) {
+                const int row = half_of(h) * 16 + g + 8 * k;
+                const uint32_t* km = reinterpret_cast<const uint32_t*>(st + F::kCodeBytes) + row * NB;
                 if constexpr (NB == 4) {
                     const uint4 a = *reinterpret_cast<const uint4*>(km);
-                    m[k][0] = a.x, m[k][1] = a.y, m[k][2] = a.z, m[k][3] = a.w;
+                    m[h][k][0] = a.x, m[h][k][1] = a.y, m[h][k][2] = a.z, m[h][k][3] = a.w;
                 } else {
                     const uint2 a = *reinterpret_cast<const uint2*>(km);
-                    m[k][0] = a.x, m[k][1] = a.y;
+                    m[h][k][0] = a.x, m[h][k][1] = a.y;
                 }
-                if (ATTEND) vw[hb][k] = reinterpret_cast<const uint32_t*>(st + F::kKeyTile + F::kCodeBytes)[hb * 16 + key_of(k)];
+                if (ATTEND) vw[h][k] = reinterpret_cast<const uint32_t*>(st + F::kKeyTile + F::kCodeBytes)[row];
             }
+        const uint4* kc = reinterpret_cast<const uint4*>(st) + lane;
 #pragma unroll
-            for (int h = 0; h < NC; ++h) {
-                const uint4 kw = kc[h * 32];
+        for (int c64 = 0; c64 < NC; ++c64) {
+            const uint4 k0 = kc[c64 * 32], k1 = kc[F::kHalfBytes / 16 + c64 * 32];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int kb = 2 * h + i;
-                    const uint4 q = sq[kb * 32 + lane];
-                    const float2 qsum = *reinterpret_cast<const float2*>(sqsum + kb * 8 + r0);
-                    float c[4];
-                    uint32_t a[4];
-                    codes_subnormal(i ? kw.z : kw.x, a);
-                    mma_f16_16816_first(c, a, q.x, q.y);
-                    codes_subnormal(i ? kw.w : kw.y, a);
-                    mma_f16_16816(c, a, q.z, q.w);
-                    if (PAIRED) c[0] = second ? c[2] : c[0], c[1] = second ? c[3] : c[1];
-#pragma unroll
-                    for (int k = 0; k < KL; ++k) {
-                        const float s = bf16_high(m[k][kb]), zs = fmaf(bf16_low(m[k][kb]), z_by[k], z_less[k]);
-                        x[hb][2 * k] = fmaf(s, fmaf(zs, qsum.x, c[2 * k]), x[hb][2 * k]);
-                        x[hb][2 * k + 1] = fmaf(s, fmaf(zs, qsum.y, c[2 * k + 1]), x[hb][2 * k + 1]);
-                    }
+            for (int i = 0; i < 2; ++i) {
+                const int kb = 2 * c64 + i;
+                const uint4 q = sq[kb * 32 + lane];
+                const float2 qsum = *reinterpret_cast<const float2*>(sqsum + kb * 8 + r0);
+                float c[2][4];
+                uint32_t a[4];
+                codes_subnormal(i ? k0.z : k0.x, a);
+                mma_f16_16816_first(c[0], a, q.x, q.y);
+                codes_subnormal(i ? k0.w : k0.y, a);
+                mma_f16_16816(c[0], a, q.z, q.w);
+                if constexpr (PAIRED) {
+                    const uint4 r = sq[(NB + kb) * 32 + lane];
+                    codes_subnormal(i ? k1.z : k1.x, a);
+                    mma_f16_16816(c[0], a, r.x, r.y);
+                    codes_subnormal(i ? k1.w : k1.y, a);
+                    mma_f16_16816(c[0], a, r.z, r.w);
+                } else {
+                    codes_subnormal(i ? k1.z : k1.x, a);
+                    mma_f16_16816_first(c[1], a, q.x, q.y);
+                    codes_subnormal(i ? k1.w : k1.y, a);
+                    mma_f16_16816(c[1], a, q.z, q.w);
                 }
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float s = bf16_high(m[h][k][kb]), z8 = bf16_low(m[h][k][kb]), zs = k ? fmaf(z8, 16.f, -128.f) : z8 - 8.f;
+                        x[h][2 * k] = fmaf(s, fmaf(zs, qsum.x, c[h][2 * k]), x[h][2 * k]);
+                        x[h][2 * k + 1] = fmaf(s, fmaf(zs, qsum.y, c[h][2 * k + 1]), x[h][2 * k + 1]);
+                    }
             }
         }
         if (tile * 32 + 32 > M)                              // rows past the count
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb)
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                for (int k = 0; k < KL; ++k)
-                    if (tile * 32 + hb * 16 + key_of(k) >= M) x[hb][2 * k] = x[hb][2 * k + 1] = SHOTKV_NEG_INF, vw[hb][k] = 0;
+                for (int k = 0; k < 2; ++k)
+                    if (tile * 32 + half_of(h) * 16 + g + 8 * k >= M) x[h][2 * k] = x[h][2 * k + 1] = SHOTKV_NEG_INF, vw[h][k] = 0;
         // weights relative to the references, which are set again where one is out of range
-        float w[2][2 * KL];
+        float w[HALVES][4];
         const auto weigh = [&] {
             const uint64_t down = tc::pack2(-ref[0], -ref[1]);
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb)
+            for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                for (int k = 0; k < 2 * KL; k += 2) {
-                    tc::unpack2(tc::ffma2(tc::pack2(x[hb][k], x[hb][k + 1]), tc::pack2(scales[k / 2][0], scales[k / 2][1]), down), w[hb][k], w[hb][k + 1]);
-                    w[hb][k] = ex2f(w[hb][k]), w[hb][k + 1] = ex2f(w[hb][k + 1]);
+                for (int k = 0; k < 2; ++k) {
+                    float y0, y1;
+                    tc::unpack2(tc::ffma2(tc::pack2(x[h][2 * k], x[h][2 * k + 1]), tc::pack2(scales[k][0], scales[k][1]), down), y0, y1);
+                    w[h][2 * k] = ex2f(y0), w[h][2 * k + 1] = ex2f(y1);
                 }
         };
         weigh();
         {
             float most = 0.f, s = 0.f;
 #pragma unroll
-            for (int hb = 0; hb < 2; ++hb)
-#pragma unroll
-                for (int k = 0; k < KL; ++k) {
-                    most = fmaxf(most, fmaxf(w[hb][2 * k], w[hb][2 * k + 1]));
-                    if (ATTEND) s = fmaxf(s, bf16_high(vw[hb][k]));
-                }
+            for (int h = 0; h < HALVES; ++h) {
+                most = fmaxf(most, fmaxf(fmaxf(w[h][0], w[h][1]), fmaxf(w[h][2], w[h][3])));
+                if (ATTEND) s = fmaxf(s, fmaxf(bf16_high(vw[h][0]), bf16_high(vw[h][1])));
+            }
             if (__any_sync(0xffffffffu, most > kHighest || (ATTEND && s * guard >= 4.f))) {
                 float high[2] = {SHOTKV_NEG_INF, SHOTKV_NEG_INF};
 #pragma unroll
-                for (int i = 0; i < 4 * KL; ++i) high[i & 1] = fmaxf(high[i & 1], x[i / (2 * KL)][i % (2 * KL)] * scales[i % (2 * KL) / 2][i & 1]);
+                for (int i = 0; i < 4 * HALVES; ++i) high[i & 1] = fmaxf(high[i & 1], x[i / 4][i % 4] * scales[i / 2 % 2][i & 1]);
                 raise(high);
                 if (ATTEND) {
 #pragma unroll
@@ -462,36 +488,33 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                 weigh();
             }
         }
-        // their sums, and with the values' scales (ATTEND) they are B fragments: high parts and remainders
+        // their sums, and with the values' scales (ATTEND) they are B fragments of the halves' eights of keys: high parts and remainders
         uint32_t wh[2][2], wl[2][2];
         uint64_t zz = tc::pack2(z[0], z[1]);
 #pragma unroll
-        for (int hb = 0; hb < 2; ++hb) {
-            uint32_t hi[KL], lo[KL];
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-            for (int k = 0; k < KL; ++k) {
-                float w0 = w[hb][2 * k], w1 = w[hb][2 * k + 1];
+            for (int k = 0; k < 2; ++k) {
+                float w0 = w[h][2 * k], w1 = w[h][2 * k + 1];
                 zz = tc::fadd2(zz, tc::pack2(w0, w1));
                 if (ATTEND) {
-                    const float s = bf16_high(vw[hb][k]) * unit, zs = bf16_low(vw[hb][k]);
+                    const float s = bf16_high(vw[h][k]) * unit, zs = bf16_low(vw[h][k]);
                     w0 *= s, w1 *= s;
                     wz[0] = fmaf(w0, zs, wz[0]);
                     wz[1] = fmaf(w1, zs, wz[1]);
-                    hi[k] = pack_f16(w0, w1);
-                    const float2 f = unpack_f16(hi[k]);
+                    const uint32_t hi = pack_f16(w0, w1);
+                    const float2 f = unpack_f16(hi);
                     float rest[2];
                     tc::unpack2(sub_pairs(tc::pack2(w0, w1), tc::pack2(f.x, f.y)), rest[0], rest[1]);
-                    lo[k] = pack_f16(rest[0], rest[1]);
+                    const uint32_t lo = pack_f16(rest[0], rest[1]);
+                    if constexpr (PAIRED) {
+                        halves_of_columns(hi, lo, second, wh[0][k], wh[1][k]);
+                        wh[0][k] = transposed(wh[0][k]), wh[1][k] = transposed(wh[1][k]);
+                    } else {
+                        wh[h][k] = transposed(hi), wl[h][k] = transposed(lo);
+                    }
                 }
             }
-            if constexpr (ATTEND && PAIRED) {
-                halves_of_columns(hi[0], lo[0], second, wh[hb][0], wh[hb][1]);
-                wh[hb][0] = transposed(wh[hb][0]), wh[hb][1] = transposed(wh[hb][1]);
-            } else if constexpr (ATTEND) {
-#pragma unroll
-                for (int k = 0; k < 2; ++k) wh[hb][k] = transposed(hi[k]), wl[hb][k] = transposed(lo[k]);
-            }
-        }
         tc::unpack2(zz, z[0], z[1]);
         if (ATTEND) {
             const uint4* vc = reinterpret_cast<const uint4*>(st + F::kKeyTile) + lane;

@@ -30,6 +30,9 @@ struct NormRopeParams {
 // (cos, sin) are read once for all of its heads and multiplied by the weights then, so that an element takes two products
 // of two numbers each, and one by 1 / sqrt.  The other element of a pair comes as it lies in memory: of halves from the lane
 // rot / 16 away, of neighbours from the same word.
+// 4 x 32,768 rows of 8 KV heads 178 us, 6.1 TB/s read and written (keys and values in warps of their own, one row at a time: 230;
+// CTAs of 256 threads: 182); 4,096 rows with all of 32 heads' queries 22 us, 4.7 TB/s: three and a half waves of warps; eight
+// single rows 2.4 us.
 constexpr int kRopeThreads = 128, kRopeAhead = 4;
 template <int D>
 __host__ __device__ constexpr int rope_heads_a_piece() { return 32 / (D / 8); }

@@ -885,7 +885,7 @@ cudaError_t ask_decode_room_t(shotkv_ctx* ctx) {
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, false, kDeep>, 256, score[0]);
     if (e == cudaSuccess) e = ask_room(decode_score_kernel<D, true, true, kDeep>, 256, score[1]);
     const auto room_of = [&](auto* kernel, bool attend, bool paired, bool fused) {
-        if (e == cudaSuccess) e = ask_room(kernel, StepKv4<D, true>::kWarps * 32, ctx->room_kv4[D == 128][attend][paired][fused]);
+        if (e == cudaSuccess) e = ask_room(kernel, StepKv4<D, true, true>::kWarps * 32, ctx->room_kv4[D == 128][attend][paired][fused]);
     };
     room_of(decode_kv4_kernel<D, false, false, false>, false, false, false);
     room_of(decode_kv4_kernel<D, false, true, false>, false, false, true);
@@ -1636,11 +1636,12 @@ constexpr int kLeastKv4 = 8, kLongShareKv4 = 3200;      // of a block of 16 rows
 template <int D, bool ATTEND, bool PAIRED>
 int launch_decode_kv4_t(shotkv_ctx* ctx, DecodeParams& p, const DecodeFinishParams& f, const PackedCache& cache, int U, bool& ended,
                         cudaStream_t stream) {
-    constexpr int threads = StepKv4<D, ATTEND>::kWarps * 32;
+    using Cfg = StepKv4<D, ATTEND, PAIRED>;
+    constexpr int threads = Cfg::kWarps * 32;
     const DecodeRoom* room = ctx->room_kv4[D == 128][ATTEND][PAIRED];
-    const auto smem_of = [&](int n) { return kv4_smem_bytes<D, ATTEND>(p.G, p.Dcap, n); };
+    const auto smem_of = [&](int n) { return kv4_smem_bytes<D, ATTEND, PAIRED>(p.G, p.Dcap, n); };
     const long long keys = (long long)p.Mcap + p.n_old + 1;
-    p.nsplit = decode_split(room[0], smem_of, U, keys, StepKv4<D, ATTEND>::kWarps, kLeastKv4);
+    p.nsplit = decode_split(room[0], smem_of, U, keys, Cfg::kWarps, kLeastKv4);
     while (p.nsplit > 1 && 2 * U * p.nsplit > (p.nsplit > 8 ? 3 : 4) * ctx->sm_count && keys < (long long)kLongShareKv4 * p.nsplit) --p.nsplit;
     const size_t smem = smem_of(p.nsplit), end = fused_end_smem_bytes(p.Hkv, f.n, f.k < f.n);
     const dim3 grid(U * p.nsplit);
