@@ -64,12 +64,12 @@ __device__ __forceinline__ Grid4 grid_of(uint32_t extreme) {
     if (__uint_as_float(s) * 15.f < R) s += 0x10000u;
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(s)));
-    const float base = 3072.5f + 0x1p-12f;
+    const float base = 2560.5f + 0x1p-12f;
     // an element that is not finite, or a range beyond float32 (fmaxf drops a NaN, the sum keeps it): the whole group reads as NaN
     const float sum = mx + neg;
     const bool fine = sum < __int_as_float(0x7f800000);
     if (!fine) inv = 0.f;
-    const float z = __uint_as_float(__float_as_uint(fine ? fmaf(-neg, inv, base) : base) & 0xfffff000u) - 3072.f;
+    const float z = __uint_as_float(__float_as_uint(fine ? fmaf(-neg, inv, base) : base) & 0xfffff000u) - 2560.f;
     Grid4 g;
     g.inv = inv;
     g.shift = base - z;
