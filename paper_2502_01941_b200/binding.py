@@ -449,7 +449,8 @@ def shotkv_decode_step_attend(ctx: Context, state: DecodeState, q, k_new, v_new,
 
 # ------------------------------------------------------------------ norm, rotation, layout; the prompt in 4 bits
 def make_rope(rows=1, rot=0, first=0, layer=0, interleaved=False, eps=1e-6) -> Rope:
-    """What shotkv_norm_rope does; it fills in the strides and the table's rows from the tensors it is given."""
+    """What shotkv_norm_rope does; each call fills in the strides and the table's rows from the tensors it is given, so calls of
+    two threads take one each."""
     return Rope(int(layer), int(first), int(rows), int(rot), int(bool(interleaved)), 0, float(eps))
 
 

@@ -827,25 +827,25 @@ cudaError_t set_kernel_attributes() {
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, kBigSmem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     };
-    std::vector<const void*> kv4;
-    const auto kv4_forms = [&](auto d) {
-        constexpr int D = decltype(d)::value;
-        for (const void* f : {(const void*)decode_kv4_kernel<D, true, false, false>, (const void*)decode_kv4_kernel<D, true, true, false>,
-                              (const void*)decode_kv4_kernel<D, true, false, true>, (const void*)decode_kv4_kernel<D, true, true, true>,
-                              (const void*)decode_kv4_kernel<D, false, false, false>, (const void*)decode_kv4_kernel<D, false, true, false>,
-                              (const void*)decode_kv4_kernel<D, false, false, true>, (const void*)decode_kv4_kernel<D, false, true, true>})
-            kv4.push_back(f);
-    };
-    kv4_forms(std::integral_constant<int, 64>());
-    kv4_forms(std::integral_constant<int, 128>());
+    const void* kv4[2][8] = {
+        {(const void*)decode_kv4_kernel<64, true, false, false>, (const void*)decode_kv4_kernel<64, true, true, false>,
+         (const void*)decode_kv4_kernel<64, true, false, true>, (const void*)decode_kv4_kernel<64, true, true, true>,
+         (const void*)decode_kv4_kernel<64, false, false, false>, (const void*)decode_kv4_kernel<64, false, true, false>,
+         (const void*)decode_kv4_kernel<64, false, false, true>, (const void*)decode_kv4_kernel<64, false, true, true>},
+        {(const void*)decode_kv4_kernel<128, true, false, false>, (const void*)decode_kv4_kernel<128, true, true, false>,
+         (const void*)decode_kv4_kernel<128, true, false, true>, (const void*)decode_kv4_kernel<128, true, true, true>,
+         (const void*)decode_kv4_kernel<128, false, false, false>, (const void*)decode_kv4_kernel<128, false, true, false>,
+         (const void*)decode_kv4_kernel<128, false, false, true>, (const void*)decode_kv4_kernel<128, false, true, true>}};
     for (const void* f : attend) in_clusters(f);
     for (const void* f : score) in_clusters(f);
-    for (const void* f : kv4) in_clusters(f);
+    for (const auto& of_size : kv4)
+        for (const void* f : of_size) in_clusters(f);
     // the fused decode step wants three CTAs of ~74 KB each on an SM: ask for the largest shared-memory carve-out
     for (const void* f : attend)
         if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
-    for (const void* f : kv4)
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+    for (const auto& of_size : kv4)
+        for (const void* f : of_size)
+            if (e == cudaSuccess) e = cudaFuncSetAttribute(f, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
     return e;
 }
 
@@ -1239,7 +1239,7 @@ int shotkv_norm_rope(shotkv_ctx* ctx, const shotkv_dims* dims, const shotkv_rope
         for (int most = ahead;; most /= 2) {
             if (dims->d == 128) rope_share<128>(heads, most, vectors, sections);
             else rope_share<64>(heads, most, vectors, sections);
-            const long long warps = (long long)((rows + ahead / vectors - 1) / (ahead / vectors)) * sections;
+            const long long warps = ((long long)rows + ahead / vectors - 1) / (ahead / vectors) * sections;
             if (most <= 2 || warps * dims->B >= 4LL * ctx->sm_count) return (warps + kRopeThreads / 32 - 1) / (kRopeThreads / 32);
         }
     };

@@ -515,6 +515,34 @@ def test_a_wait_that_gives_up_leaves_the_context_usable(ctx, shape):
     t.check(True, [(0, 0), (shape[0] - 1, shape[1] - 1)])
 
 
+def test_both_ways_of_marshalling(ctx, monkeypatch):
+    """Through the module and through ctypes: the same results, and the same exceptions."""
+    from paper_2502_01941_b200 import binding
+    import test_norm_rope_gpu as N
+    assert binding._native is not None
+    results = []
+    for native in (binding._native, None):
+        monkeypatch.setattr(binding, "_native", native)
+        s, r = Step(ctx, 2, 1, 2, 4, 64, 90, 10), N.Layer(2, 1, 4, 2, 64, 30, 5, 0, 30, 64, all_q=True)
+        Kc, Vc = torch.zeros_like(s.K), torch.zeros_like(s.V)
+        r.run(ctx)
+        skv.shotkv_unpack_kv4(ctx, s.dims, s.K4, s.V4, s.count, 90, Kc, Vc)
+        s.run(True)
+        first = (s.out.clone(), s.acc.clone())
+        s.st.T = s.st.n_dec = 10
+        s.run(False)
+        results.append([s.K4, s.V4, Kc, Vc, *first, s.acc, r.K, r.V, r.Qwin, r.q_out])
+        for call in (lambda: skv.shotkv_compact_kv4(ctx, s.dims, s.K, s.V, None, s.count, 90, s.K4.cpu(), s.V4),
+                     lambda: skv.shotkv_unpack_kv4(ctx, s.dims, s.K4.cpu(), s.V4, s.count, 90, Kc, Vc),
+                     lambda: skv.shotkv_decode_step_kv4(ctx, s.st, s.q, s.k, s.v, s.K4.cpu(), s.count)):
+            with pytest.raises(ValueError, match="K4"):
+                call()
+        with pytest.raises(TypeError, match="positions"):
+            skv.shotkv_norm_rope(ctx, r.dims, r.rope, r.q, r.k, r.v, r.wq, r.wk, r.table, torch.zeros(2, 30, device="cuda"), r.Qwin, r.K, r.V)
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+
+
 def test_results_do_not_change_from_call_to_call(ctx):
     for shape in ((1, 1, 8, 4, 128, 1500, 100), (8, 8, 8, 4, 64, 200, 30)):
         outs = []
