@@ -4,6 +4,7 @@
 
 #include "decode.cuh"
 #include "kv4.cuh"
+#include "ring.cuh"
 #include "score_tc.cuh"
 
 namespace shotkv {
@@ -189,9 +190,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         if (ATTEND) bulk_load(st + F::kKeyTile, Vt_u + (size_t)tile * F::kValueTile, F::kValueTile, bar);
     };
     // The first are asked for before the kept count is there: tiles below the cap can be read.
-#pragma unroll
-    for (int k = 0; k < NS; ++k)
-        if (first_tile + k * step < all_tiles) fetch(first_tile + k * step, k);
+    TileRing<NS> ahead(first_tile, step);
+    ahead.ask(all_tiles, fetch);
     if (FUSED || p.nsplit > 1) cluster_wait();               // all CTAs of the cluster have begun: their memory may be written to
     if (appends)                                             // decode entry n_old
         (tid < VPR ? Kd_u + (size_t)p.n_old * VPR + tid : Vd_u + (size_t)p.n_old * VPR + (tid - VPR))[0] = fresh_row;
@@ -363,26 +363,18 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     Under under = codes_under();
     under.k1024 |= (uint32_t)p.nsplit >> 31, under.k1032 |= (uint32_t)p.nsplit >> 31;
     float guard = 0x1p110f;                                  // `unit` once it is set, until then a number that sets it
-    int stage = 0;
-    uint32_t parity = 0;
     // The same answer in all lanes; `limit` cycles at most.
-    const auto landed = [&](long long limit) {
+    const auto landed = [&](int stage, uint32_t parity, long long limit) {
         bool there = tc::mbar_try(smem_u32(bars + stage), parity);
         if (__all_sync(0xffffffffu, there)) return true;
         there = there || await_messages(bars + stage, p.err, limit, parity);
         return (bool)__all_sync(0xffffffffu, there);
     };
-    const auto advance = [&] {
-        stage = stage + 1 == NS ? 0 : stage + 1;
-        if (stage == 0) parity ^= 1;
-    };
-    int tile = first_tile;
-    bool lost = false;                                       // a wait gave up: the warp goes on with what it has
 #pragma unroll 1
-    for (; tile < tiles; tile += step) {
-        lost = !landed(p.wait_cycles);
-        if (lost) break;
-        const unsigned char* st = mine + stage * Cfg::kStageBytes;
+    while (ahead.tile < tiles) {
+        if (!landed(ahead.stage, ahead.parity, p.wait_cycles)) break;     // the warp goes on with what it has
+        const int tile = ahead.tile;
+        const unsigned char* st = mine + ahead.stage * Cfg::kStageBytes;
         // of this lane's halves, logits of keys g (x[.][0..1], still to be scaled) and g + 8 (x[.][2..3]), and the values' words
         float x[HALVES][4] = {};
         uint32_t m[HALVES][2][NB], vw[HALVES][2];
@@ -539,17 +531,9 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             }
         }
         __syncwarp();                                       // every lane has read the stage the next copy overwrites
-        if (tile + NS * step < tiles) fetch(tile + NS * step, stage);
-        advance();
+        ahead.next(tiles, fetch);
     }
-    // What was asked for and not used, beyond the kept rows or after a wait that gave up, lands too, before its place is used
-    // again or the CTA ends.
-#pragma unroll 1
-    for (int k = 0; k < NS; ++k, tile += step)
-        if (tile < all_tiles && (tile < first_tile + NS * step || tile < tiles)) {
-            landed(lost ? tc::kWaitCycles : p.wait_cycles);
-            advance();
-        }
+    ahead.land(all_tiles, tiles, landed);
 
     // ---- the warp's rows
 #pragma unroll
