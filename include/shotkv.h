@@ -395,8 +395,8 @@ SHOTKV_API uint64_t shotkv_repaired_items(const shotkv_ctx* ctx);
  * memory barriers; the CTAs of a cluster in the reduction and the decode steps wait for one another's
  * messages.  Every such wait is bounded: after `cycles` SM clock cycles (default 4e9, about
  * two seconds) the waiting warp gives up, raises its CTA's abort flag and a host-visible error
- * word, all roles leave their loops, copies and messages in flight are waited for (bounded again),
- * tensor memory is released and the kernel returns.  The next call on the context then returns
+ * word, all roles leave their loops, copies and messages in flight are waited for (about two seconds at most, whatever
+ * the limit: they write into the CTA's memory), tensor memory is released and the kernel returns.  The next call on the context then returns
  * SHOTKV_ERR_TIMEOUT once (the outputs of the call that gave up are invalid); the call after
  * that proceeds normally.  A decode state whose step gave up is invalid as a whole: initialise it again.
  * shotkv_set_wait_limit changes the limit for later launches of this context (0 restores the default).  */

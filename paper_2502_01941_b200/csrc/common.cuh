@@ -4,6 +4,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "ring.cuh"
+
 namespace shotkv {
 
 constexpr int kWarp = 32;
@@ -158,12 +160,12 @@ __device__ __forceinline__ bool await_messages(unsigned long long* bar, int* err
 }
 // For single threads whose wait gave up, at their end: keeps their CTA, whose memory the others write to, until all
 // other threads of the cluster have ended or are here too (every wait of theirs ends), and until what they sent has
-// landed, if it does within the limit.  `bar`, `more`: the barriers waited for in vain, or NULL.
-__device__ __forceinline__ void outlive_messages(unsigned long long* bar, unsigned long long* more, int* err, long long limit) {
+// landed (kLandCycles at most, whatever limit the wait had).  `bar`, `more`: the barriers waited for in vain, or NULL.
+__device__ __forceinline__ void outlive_messages(unsigned long long* bar, unsigned long long* more, int* err) {
     asm volatile("barrier.cluster.arrive.release;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire;" ::: "memory");
-    if (bar) await_messages(bar, err, limit);
-    if (more) await_messages(more, err, limit);
+    if (bar) await_messages(bar, err, kLandCycles);
+    if (more) await_messages(more, err, kLandCycles);
 }
 
 // Self-test of that, for the host to run on demand: a cluster of two CTAs of one warp.  The first expects two words;
@@ -189,7 +191,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(32) message_wait_sel
     }
     const bool ok = await_messages(&arrived, err, limit);
     report[0] = ok;
-    if (!ok) outlive_messages(&arrived, nullptr, err, limit);
+    if (!ok) outlive_messages(&arrived, nullptr, err);
     report[1] = *(volatile float*)&words[0] == 1.f && *(volatile float*)&words[1] == 2.f;
 }
 

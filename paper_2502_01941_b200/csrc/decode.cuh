@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(256) decode_score_kernel(const DecodeParams p,
             else p.partial[(size_t)u * p.Dcap + j] = s;
         });
         const bool all = !FUSED || fused_finish<D, 256>(end, f, bl, first_cta + rank, ctas, p);
-        if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err, p.wait_cycles);
+        if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err);
     } else {
         // (entry_weights here takes registers of a CTA on the SM: 448 units of 3,276 keys, d = 128, 61.5 -> 83.9 us a step)
         for (int j0 = warp * 32; j0 < n; j0 += 256) {
@@ -605,7 +605,7 @@ __device__ __forceinline__ void finish_attend(const DecodeParams& p, const Decod
         else p.partial[(size_t)part.u * p.Dcap + j] = s;
     });
     const bool all = !FUSED || fused_finish<D, NT>(end, f, part.bl, part.first_cta + part.rank, part.ctas, p);
-    if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err, p.wait_cycles);
+    if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err);
 }
 
 // Shared-memory staging of the fused step: every warp owns a ring of kStages stages, a stage

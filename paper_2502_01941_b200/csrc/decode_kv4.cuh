@@ -592,7 +592,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             else p.partial[(size_t)u * p.Dcap + j] = s;
         });
         const bool all = !FUSED || fused_finish<D, NW * 32>(end, f, bl, first_cta + rank, ctas, p);
-        if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err, p.wait_cycles);
+        if (!(ok && all)) outlive_messages(ok ? nullptr : arrived, all ? nullptr : end.arrived, p.err);
     }
 }
 

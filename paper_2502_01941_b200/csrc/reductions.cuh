@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kReduceThreads, ROWS == 128 || AHEAD < 4 ? 4 :
         scores[i] = s;
         return s;
     });
-    if (!ok) outlive_messages(&arrived, nullptr, err, wait_cycles);
+    if (!ok) outlive_messages(&arrived, nullptr, err);
 }
 
 // Score(s_i) from per-token importance.  Latency-bound while the importances come from L2, so what counts is how

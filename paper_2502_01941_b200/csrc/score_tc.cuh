@@ -457,19 +457,22 @@ __device__ __forceinline__ void producer_role(const Pipe<Cfg>& pp, const CUtenso
             }
         }
     }
-    if (!ok) {
-        // aborting: give the copies already issued a bounded time to land before the CTA ends
-        const long long t0 = clock64();
-        int s = stage;
-        uint32_t ph = ephase;
-        for (int k = 0; k < outstanding; ++k) {
-            if (--s < 0) {
-                s = NST - 1;
-                ph ^= 1;
-            }
-            while (!mbar_try(pp.full(s), ph ^ 1) && clock64() - t0 < p.wait_cycles) {
-            }
+    // The copies issued land before the CTA ends, the queries' too, in kLandCycles at most: where a role has given up, this one
+    // or another, nobody else waits for them.
+    const long long t0 = clock64();
+    const auto land = [&](uint32_t bar, uint32_t parity) {
+        while (!mbar_try(bar, parity) && clock64() - t0 < kLandCycles) {
         }
+    };
+    if (cur_u >= 0) land(pp.qfull(), qephase);
+    int s = stage;
+    uint32_t ph = ephase;
+    for (int k = 0; k < outstanding; ++k) {
+        if (--s < 0) {
+            s = NST - 1;
+            ph ^= 1;
+        }
+        land(pp.full(s), ph ^ 1);
     }
 }
 

@@ -96,6 +96,26 @@ def test_every_copy_lands(driver, limit, late_by):
     assert ran.value > 10000
 
 
+def test_what_is_in_flight_is_waited_for_whatever_the_limit():
+    """In the kernels that copy by descriptor and in those that send messages: the waits at a CTA's end, for what will still be
+    written into its memory, do not have the limit that a program sets, and the copies are waited for when another role gave up too."""
+    def body(f, name):
+        text = open(os.path.join(CSRC, f)).read()
+        start = text.index("{", text.index(name + "("))
+        depth, end = 1, start + 1
+        while depth:
+            depth += {"{": 1, "}": -1}.get(text[end], 0)
+            end += 1
+        return text[start:end]
+
+    message = body("common.cuh", "void outlive_messages")
+    assert message.count("kLandCycles") == 2 and "limit)" not in message
+    producer = body("score_tc.cuh", "void producer_role")
+    last = producer[producer.rindex("tma_load_3d"):]
+    assert "kLandCycles" in last and "p.wait_cycles" not in last
+    assert "if (!ok)" not in last and "land(pp.qfull()" in last and "land(pp.full(s)" in last
+
+
 def test_the_step_goes_through_it():
     """The kernel has no ring of its own beside the one tested here."""
     text = open(os.path.join(CSRC, "decode_kv4.cuh")).read()
