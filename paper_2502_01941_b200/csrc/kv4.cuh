@@ -53,20 +53,24 @@ struct Grid4 {
 // The scale is the least bf16 number s with 15 s >= R = max(range, max|x| / 16, 15 * 2^-100): sixteen steps reach
 // over the range, the grid of multiples of s is no finer than bf16 itself near the group's largest element (so that z is
 // whole and below 256, exact in bf16), and nothing is divided by zero.  c + z = floor(x / s + 1/2).
+// The range is that of the numbers themselves, which 32 bits may round.  15 s has 12 bits, so it is on the same side of the range as of the
+// rounded one, unless it is the rounded one: then what was rounded off decides.  (It is exact in 32 bits: of max and -min the greater is
+// no smaller in magnitude than the other.)
 // A quotient x / s of bf16 numbers that the rule admits (|x / s| <= 240) is a half-integer or 2^-10 away from every one, so
 // a quotient off by less (1 / s to 2^-22, the sum rounded to 2^-12) is rounded the right way once 2^-12 is added.
 __device__ __forceinline__ Grid4 grid_of(uint32_t extreme) {
     const float mx = __uint_as_float(extreme << 16), neg = __uint_as_float(extreme & 0xffff0000u);    // max and -min
-    const float R = fmaxf(fmaxf(mx + neg, fmaxf(mx, neg) * 0.0625f), 15.f * 0x1p-100f);
+    const float sum = mx + neg, most = fmaxf(mx, neg), rest = fminf(mx, neg) - (sum - most);
+    const float R = fmaxf(fmaxf(sum, most * 0.0625f), 15.f * 0x1p-100f);
     // 1/15 rounded down, and the product down to bf16; then up until it is enough (products with 15 are exact)
     uint32_t s = __float_as_uint(R * 0x1.11111p-4f) & 0xffff0000u;
     if (__uint_as_float(s) * 15.f < R) s += 0x10000u;
     if (__uint_as_float(s) * 15.f < R) s += 0x10000u;
+    if (__uint_as_float(s) * 15.f == sum && rest > 0.f) s += 0x10000u;
     float inv;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(__uint_as_float(s)));
     const float base = 2560.5f + 0x1p-12f;
     // an element that is not finite, or a range beyond float32 (fmaxf drops a NaN, the sum keeps it): the whole group reads as NaN
-    const float sum = mx + neg;
     const bool fine = sum < __int_as_float(0x7f800000);
     if (!fine) inv = 0.f;
     const float z = __uint_as_float(__float_as_uint(fine ? fmaf(-neg, inv, base) : base) & 0xfffff000u) - 2560.f;
