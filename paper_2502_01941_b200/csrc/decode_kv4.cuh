@@ -90,8 +90,8 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 //     largest element to [2^14, 2^15), which leaves elements down to 2^-31 of it exact.  A logit is the sum over groups of
 //     s (S + (z - 8) times the sum of q's 32 elements).
 //   O^T[16 dims x 8 rows] += c^T . w^T with w = p s_v, p = 2^(logit - reference): the accumulator of S, transposed 8 by 8, is
-//     the other operand, an f16 pair (high part and remainder: 2^-22 of w, or 2^-35 of the row's largest where that is more).  z
-//     is added once a row: sum of w z_v.
+//     the other operand, an f16 pair (high part and remainder: 2^-22 of w, or half of f16's least step, 2^-25).  z is added once a
+//     row: sum of w z_v.
 // PAIRED, for groups of up to four rows: the columns 4 .. 7 are the same rows again.  The remainders are in these columns of the one
 // operand whose columns 0 .. 3 are the high parts, so that one product does for both, and the lanes of columns 0 .. 3 have the
 // logits of one half of a tile, those of columns 4 .. 7 of the other.  (8 sequences x 32 layers, 3,276 rows, 145
@@ -99,8 +99,10 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 //
 // f16 ends at 65504, so both factors are kept in range by references that change seldom: a row's reference is 2^10 below its
 // maximum when it was last set and is set again by a tile whose p would exceed 2^13, and the values' scales are multiplied by a
-// power of two that takes the largest of the first tile to [1, 2) and is set again when one exceeds 4.  One vote a tile
-// decides that neither has happened.  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
+// power of two that takes the largest of the first tile to [1, 2) and is set again by a tile with a scale outside [2^-8, 4); if the tile's
+// own scales are that far apart, its rows of small scale are added by themselves.  So a weight is off by no more than 2^-27 of the row's
+// largest (2^-35 where the scales are alike), whatever the others' values are.  One vote a tile
+// decides that nothing of this has happened.  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
 // products are summed for themselves and then added: one sum for all of a warp's 26 tiles left the outputs 4.2e-6 off in the
 // 2-norm, so they are 5.5e-7 off (elementary operations in 32 bits: 9.3e-7).
 //
@@ -355,14 +357,40 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     // at the power cap where this takes 208).
     constexpr int HALVES = PAIRED ? 1 : 2;                   // of a tile, that a lane has keys of
     const auto half_of = [&](int h) { return PAIRED ? (int)second : h; };
-    float unit = 1.f;                                        // O and wz are in units of 1 / unit, of odd dimensions O in a sixteenth of it
-    if (ATTEND)
+    // A tile's weights times scales are in units of back = 1 / unit; the first tile of all sets them.
+    float unit = 0x1p100f, back = 0x1p-100f;
+    if (ATTEND)                                              // odd dimensions' are sixteen times as much from here on
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) O[mt][2] *= 16.f, O[mt][3] *= 16.f;
     // in registers that the compiler cannot make anew for each use
     Under under = codes_under();
     under.k1024 |= (uint32_t)p.nsplit >> 31, under.k1032 |= (uint32_t)p.nsplit >> 31;
-    float guard = 0x1p110f;                                  // `unit` once it is set, until then a number that sets it
+    // Scales of 2^-8 to 4 in these units, as a value's word less the least of them: 0 to kSpan - 1.
+    constexpr uint32_t kSpan = 10u << 23;
+    const auto above = [&](uint32_t word) { return word - (__float_as_uint(back) - (8u << 23)); };
+    // The value in lane `src` of those that hold the first of the query rows (its half of the tile h, where a lane has both; row g + 8 k
+    // of it) times its weights, in plain multiply-adds.
+    const auto add_row = [&](const unsigned char* st, int src, int h, int k, float w0, float w1, uint32_t word) {
+        const int r = src >> 2, half = PAIRED ? src >> 1 & 1 : h, from = src + (PAIRED ? t4 & 1 : t4);
+        w0 = __shfl_sync(0xffffffffu, w0, from), w1 = __shfl_sync(0xffffffffu, w1, from);
+        word = __shfl_sync(0xffffffffu, word, src);
+        const float s = bf16_high(word), z8 = bf16_low(word) - 8.f;
+        const uint4* vc = reinterpret_cast<const uint4*>(st + F::kKeyTile + half * F::kHalfBytes) + 4 * g + (r >> 1);
+        if (second) return;                                  // its columns are the remainders of the same rows
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const uint4 v4 = vc[c * 32];
+            const uint32_t v[4] = {v4.x, v4.y, v4.z, v4.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float x = (float)(v[i] >> (4 * (e + 2 * k) + 16 * (r & 1)) & 15u) + z8, y = s * (e ? 16.f * x : x);
+                    O[c * 4 + i][2 * e] = fmaf(w0, y, O[c * 4 + i][2 * e]);
+                    O[c * 4 + i][2 * e + 1] = fmaf(w1, y, O[c * 4 + i][2 * e + 1]);
+                }
+        }
+    };
     // The same answer in all lanes; `limit` cycles at most.
     const auto landed = [&](int stage, uint32_t parity, long long limit) {
         bool there = tc::mbar_try(smem_u32(bars + stage), parity);
@@ -435,7 +463,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                 for (int k = 0; k < 2; ++k)
-                    if (tile * 32 + half_of(h) * 16 + g + 8 * k >= M) x[h][2 * k] = x[h][2 * k + 1] = SHOTKV_NEG_INF, vw[h][k] = 0;
+                    if (tile * 32 + half_of(h) * 16 + g + 8 * k >= M) x[h][2 * k] = x[h][2 * k + 1] = SHOTKV_NEG_INF, vw[h][k] = __float_as_uint(back);
         // weights relative to the references, which are set again where one is out of range
         float w[HALVES][4];
         const auto weigh = [&] {
@@ -451,33 +479,44 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         };
         weigh();
         {
-            float most = 0.f, s = 0.f;
+            float most = 0.f;
+            uint32_t far = 0;
 #pragma unroll
             for (int h = 0; h < HALVES; ++h) {
                 most = fmaxf(most, fmaxf(fmaxf(w[h][0], w[h][1]), fmaxf(w[h][2], w[h][3])));
-                if (ATTEND) s = fmaxf(s, fmaxf(bf16_high(vw[h][0]), bf16_high(vw[h][1])));
+                if (ATTEND) far = max(far, max(above(vw[h][0]), above(vw[h][1])));
             }
-            if (__any_sync(0xffffffffu, most > kHighest || (ATTEND && s * guard >= 4.f))) {
+            if (__any_sync(0xffffffffu, most > kHighest || far >= kSpan)) {
                 float high[2] = {SHOTKV_NEG_INF, SHOTKV_NEG_INF};
 #pragma unroll
                 for (int i = 0; i < 4 * HALVES; ++i) high[i & 1] = fmaxf(high[i & 1], x[i / 4][i % 4] * scales[i / 2 % 2][i & 1]);
                 raise(high);
-                if (ATTEND) {
+                weigh();
+                if (ATTEND && __any_sync(0xffffffffu, far >= kSpan)) {
+                    float s = 0.f;                           // the greatest scale (of those that are numbers)
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            if (tile * 32 + half_of(h) * 16 + g + 8 * k >= M) vw[h][k] = 0;
+                            s = fmaxf(s, bf16_high(vw[h][k]));
+                        }
 #pragma unroll
                     for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
-                    const int e = min(max((int)(__float_as_uint(s) >> 23), 67), 250);      // its exponent
-                    float next = __uint_as_float((uint32_t)(254 - e) << 23);
-                    if (guard == unit) next = fminf(unit, next);
-                    const float al = next / unit;
+                    const uint32_t e = min(max(__float_as_uint(s) >> 23, 27u), 250u);      // its exponent
+                    unit = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
+                    // a row whose scale is small beside it is added by itself
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) wz[r] *= al;
+                    for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-                    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) O[mt][c] *= al;
-                    unit = guard = next;
+                        for (int k = 0; k < 2; ++k) {
+                            const bool alone = vw[h][k] != 0 && (int)above(vw[h][k]) < 0;
+                            uint32_t lanes = __ballot_sync(0xffffffffu, alone) & (PAIRED ? 0x55555555u : 0x11111111u);
+#pragma unroll 1
+                            for (; lanes; lanes &= lanes - 1) add_row(st, __ffs(lanes) - 1, h, k, w[h][2 * k], w[h][2 * k + 1], vw[h][k]);
+                            if (alone) vw[h][k] = 0;
+                        }
                 }
-                weigh();
             }
         }
         // their sums, and with the values' scales (ATTEND) they are B fragments of the halves' eights of keys: high parts and remainders
@@ -490,10 +529,10 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                 float w0 = w[h][2 * k], w1 = w[h][2 * k + 1];
                 zz = tc::fadd2(zz, tc::pack2(w0, w1));
                 if (ATTEND) {
-                    const float s = bf16_high(vw[h][k]) * unit, zs = bf16_low(vw[h][k]);
-                    w0 *= s, w1 *= s;
-                    wz[0] = fmaf(w0, zs, wz[0]);
-                    wz[1] = fmaf(w1, zs, wz[1]);
+                    const float s = bf16_high(vw[h][k]), sz = s * bf16_low(vw[h][k]), su = s * unit;
+                    wz[0] = fmaf(w0, sz, wz[0]);
+                    wz[1] = fmaf(w1, sz, wz[1]);
+                    w0 *= su, w1 *= su;
                     const uint32_t hi = pack_f16(w0, w1);
                     const float2 f = unpack_f16(hi);
                     float rest[2];
@@ -510,6 +549,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         tc::unpack2(zz, z[0], z[1]);
         if (ATTEND) {
             const uint4* vc = reinterpret_cast<const uint4*>(st + F::kKeyTile) + lane;
+            const uint64_t back2 = tc::pack2(back, back);
 #pragma unroll
             for (int h = 0; h < NC; ++h) {
                 const uint4 v0 = vc[h * 32], v1 = vc[F::kHalfBytes / 16 + h * 32];
@@ -525,8 +565,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     if (!PAIRED) mma_f16_16816(c, a, wl[1][0], wl[1][1]);
                     mma_f16_16816(c, a, wh[1][0], wh[1][1]);
                     float(&o)[4] = O[h * 4 + i];
-                    tc::unpack2(tc::fadd2(tc::pack2(o[0], o[1]), tc::pack2(c[0], c[1])), o[0], o[1]);
-                    tc::unpack2(tc::fadd2(tc::pack2(o[2], o[3]), tc::pack2(c[2], c[3])), o[2], o[3]);
+                    tc::unpack2(tc::ffma2(tc::pack2(c[0], c[1]), back2, tc::pack2(o[0], o[1])), o[0], o[1]);
+                    tc::unpack2(tc::ffma2(tc::pack2(c[2], c[3]), back2, tc::pack2(o[2], o[3])), o[2], o[3]);
                 }
             }
         }
@@ -550,7 +590,6 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     constexpr int kPitch = NS * Cfg::kStageBytes / 4;       // floats
     float* sO = reinterpret_cast<float*>(ring);
     if (ATTEND) {
-        const float back = 1.f / unit;
 #pragma unroll
         for (int r = 0; r < 2; ++r)
 #pragma unroll
@@ -563,7 +602,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     for (int e = 0; e < 2; ++e) {
                         float x = O[h * 4 + i][2 * e + r];
                         if (PAIRED) x += __shfl_xor_sync(0xffffffffu, x, 2);
-                        v[2 * i + e] = (e ? fmaf(x, 0.0625f, wz[r]) : x + wz[r]) * back;
+                        v[2 * i + e] = e ? fmaf(x, 0.0625f, wz[r]) : x + wz[r];
                     }
                 if (!second) {
                     *reinterpret_cast<float4*>(o) = make_float4(v[0], v[1], v[2], v[3]);

@@ -8,7 +8,7 @@ import torch
 
 import kv4_reference as R
 import paper_2502_01941_b200 as skv
-from test_kv4_gpu import f64, packed
+from test_kv4_gpu import Step, f64, normal, packed
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +74,91 @@ def test_the_scale_goes_by_the_range_of_the_numbers_themselves(ctx, d):
                 scale, whole = exact_grid(rows[r, g])
                 assert Fraction(s[r, at]) == scale, ends[r]
                 assert (c[r, g] + z[r, g]).tolist() == whole and z[r, at] == min(whole) + 8, ends[r]
+
+
+# ------------------------------------------------------------------------------------------------ the steps
+def check_outputs(s, scores=True):
+    """A step's outputs and scores against 64 bits.  The allowance is kv4_reference.step's for sums in 32 bits, and for a weight's
+    place in the product: it enters with its value's scale as two f16 numbers, the second of them off by 2^-25 in units of a power
+    of two that is no more than the largest scale and no more than 2^8 times the row's own, while the row's largest weight is
+    2^10 or more: 2^-35 of that weight and the largest scale, or 2^-27 of it and the own scale, times a code of up to 8."""
+    m, n = s.M, s.n_old + 1
+    acc, out = s.acc.cpu().numpy(), s.out.cpu().numpy()
+    for b in range(s.B):
+        for l in range(s.L):
+            kk, kv = f64(s.K[b, l]), f64(s.V[b, l])
+            kd, vd = f64(s.Kd[b, l, :, :n]), f64(s.Vd[b, l, :, :n])
+            scale = R.quantise(kv)[1]                                   # [Hkv, M]
+            keys = np.concatenate([R.values_of(kk, True), kd], 1)
+            w, w_off, o, o_off = R.step(f64(s.q[b, l]), keys, np.concatenate([R.values_of(kv, False), vd], 1), m,
+                                        np.concatenate([R.sizes_of(kk, True), np.abs(kd)], 1),
+                                        np.concatenate([R.sizes_of(kv, False), np.abs(vd)], 1))
+            x = np.einsum("hgd,htd->hgt", f64(s.q[b, l]).reshape(s.Hkv, s.G, s.d), keys) / np.sqrt(s.d)
+            p = np.exp(x - x.max(-1, keepdims=True))
+            largest = 1 / p.sum(-1)                                     # [Hkv, G]
+            product = 8 * np.minimum(2.0 ** -35 * scale.max(-1, keepdims=True), 2.0 ** -27 * scale).sum(-1)
+            o_off = o_off + (largest * product[:, None]).reshape(-1, 1)
+            assert np.isfinite(out[b, l]).all()
+            err = np.abs(out[b, l] - o)
+            assert np.all(err <= o_off), f"outputs of {b}, {l}: off by {(err / o_off).max()} of what they may be"
+            if scores:
+                old = np.append(s.before[b, l, :n - 1], 0.0)
+                assert np.all(np.abs(acc[b, l, :n] - (old + w)) <= w_off + 2.0 ** -22 * (old + w)), "scores"
+
+
+def bf(t):
+    return t.to(torch.bfloat16).contiguous()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 7])
+@pytest.mark.parametrize("exponent", [6, 10, 20, 28, 32, 60, -10, -28, -60, -90])
+@pytest.mark.parametrize("every", [1, 3, 40])
+def test_values_far_from_the_others_that_have_no_weight(ctx, every, exponent, G, d):
+    """Rows (all of a block of 40, or every third or fortieth) whose values are larger or smaller by a power of two and whose keys point
+    away from every query: the others' outputs are as they would be alone."""
+    M = 333
+    K, V, q = (normal(i, 1, 2, 2, r, d).float() for i, r in ((1, M), (2, M), (3, G)))
+    far = torch.zeros(M, dtype=torch.bool, device="cuda")
+    far[slice(60, 100) if every == 1 else slice(2, None, every)] = True
+    V[:, :, :, far] *= 2.0 ** exponent
+    q[..., 0], K[..., 0] = 20.0, 0.0
+    K[:, :, :, far], K[:, :, :, far, 0] = 0.0, -60.0
+    s = Step(ctx, 1, 2, 2, G, d, M, 30, counts=np.full((1, 2), M, np.int32), keys=bf(K), values=bf(V), q=bf(q.reshape(1, 2, 2 * G, d)))
+    s.run(True)
+    check_outputs(s)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 8])
+@pytest.mark.parametrize("M", [31, 700])
+def test_values_of_every_size_at_once(ctx, M, G, d):
+    """Scales from 2^-70 to 2^40 from row to row, weights and scales independent."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    V = normal(2, 1, 1, 2, M, d).float() * torch.exp2(110 * torch.rand(1, 1, 2, M, 1, generator=g, device="cuda") - 70)
+    s = Step(ctx, 1, 1, 2, G, d, M, 20, counts=np.full((1, 1), M, np.int32), values=bf(V))
+    s.run(True)
+    check_outputs(s)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 8])
+@pytest.mark.parametrize("exponent", [-40, -62, -80, -95, 40, 90])
+def test_values_of_any_one_size(ctx, exponent, G, d):
+    """All values, the entries' too, are the same power of two smaller or larger than one: so are the outputs."""
+    M = 200
+    s = Step(ctx, 1, 1, 2, G, d, M, 20, counts=np.full((1, 1), M, np.int32), values=bf(normal(2, 1, 1, 2, M, d).float() * 2.0 ** exponent))
+    for t in (s.Vd, s.v):
+        t *= 2.0 ** exponent
+    s.run(True)
+    check_outputs(s)
+
+
+def test_rows_of_zeros_among_values(ctx):
+    """A row of zeros has the least scale there is; it adds nothing, and does not disturb the others."""
+    V = normal(2, 1, 1, 2, 300, 128)
+    V[:, :, :, ::7] = 0
+    V[:, :, :, 64:96] = 0
+    s = Step(ctx, 1, 1, 2, 4, 128, 300, 20, counts=np.full((1, 1), 300, np.int32), values=V)
+    s.run(True)
+    check_outputs(s)
