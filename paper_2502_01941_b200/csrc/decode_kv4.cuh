@@ -118,7 +118,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     using F = Kv4<D>;
     constexpr int NB = D / 32, NC = D / 64, VPR = D / 8, MT = D / 16;
     constexpr int NW = Cfg::kWarps, NS = Cfg::kStages;
-    constexpr float kLift = 10.f, kHighest = 8192.f, kUnset = -1e30f;
+    constexpr float kLift = 10.f, kHighest = 8192.f, kUnset = -3.402823466e38f, kCoarse = 0x1p22f;
     extern __shared__ __align__(128) unsigned char dsm[];
     unsigned char* ring = dsm;                               // [NW][NS][keys | values]; later each warp's outputs
     uint4* sq = reinterpret_cast<uint4*>(ring + Cfg::kRingBytes + Cfg::kBarBytes);   // [1, PAIRED 2][NB][32 lanes] the queries as B fragments, f16
@@ -254,7 +254,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             float m = high[r];
 #pragma unroll
             for (int o = kFirstLane; o <= 16; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-            const float up = fmaxf(ref[r], m - kLift);
+            // (a logit of 2^27 or more has steps of 16 and more: it is its own reference)
+            const float up = fmaxf(ref[r], fabsf(m) < 0x1p27f ? m - kLift : m);
             const float al = ex2f(ref[r] - up);
             ref[r] = up;
             z[r] *= al;
@@ -362,6 +363,16 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     if (ATTEND)                                              // odd dimensions' are sixteen times as much from here on
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) O[mt][2] *= 16.f, O[mt][3] *= 16.f;
+    // From 2^22 on a logit's own rounding counts: as a multiply-add its weight would be that of the exact product, apart from the
+    // reference by up to half a step of 32 bits.  So a warp that has met one so large looks at every tile again, where logits
+    // are rounded before the reference is subtracted, as the entries' are.
+    const auto coarse = [&] {
+        bool large = false;
+#pragma unroll
+        for (int r = 0; r < 2; ++r) large |= ref[r] != kUnset && fabsf(ref[r]) >= kCoarse;
+        return (bool)__any_sync(0xffffffffu, large);
+    };
+    float highest = coarse() ? -1.f : kHighest;              // what a tile's weights may be: below zero, each is looked at again
     // in registers that the compiler cannot make anew for each use
     Under under = codes_under();
     under.k1024 |= (uint32_t)p.nsplit >> 31, under.k1032 |= (uint32_t)p.nsplit >> 31;
@@ -466,7 +477,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     if (tile * 32 + half_of(h) * 16 + g + 8 * k >= M) x[h][2 * k] = x[h][2 * k + 1] = SHOTKV_NEG_INF, vw[h][k] = __float_as_uint(back);
         // weights relative to the references, which are set again where one is out of range
         float w[HALVES][4];
-        const auto weigh = [&] {
+        {
             const uint64_t down = tc::pack2(-ref[0], -ref[1]);
 #pragma unroll
             for (int h = 0; h < HALVES; ++h)
@@ -476,8 +487,7 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     tc::unpack2(tc::ffma2(tc::pack2(x[h][2 * k], x[h][2 * k + 1]), tc::pack2(scales[k][0], scales[k][1]), down), y0, y1);
                     w[h][2 * k] = ex2f(y0), w[h][2 * k + 1] = ex2f(y1);
                 }
-        };
-        weigh();
+        }
         {
             float most = 0.f;
             uint32_t far = 0;
@@ -486,12 +496,18 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                 most = fmaxf(most, fmaxf(fmaxf(w[h][0], w[h][1]), fmaxf(w[h][2], w[h][3])));
                 if (ATTEND) far = max(far, max(above(vw[h][0]), above(vw[h][1])));
             }
-            if (__any_sync(0xffffffffu, most > kHighest || far >= kSpan)) {
+            if (__any_sync(0xffffffffu, most > highest || far >= kSpan)) {
                 float high[2] = {SHOTKV_NEG_INF, SHOTKV_NEG_INF};
 #pragma unroll
-                for (int i = 0; i < 4 * HALVES; ++i) high[i & 1] = fmaxf(high[i & 1], x[i / 4][i % 4] * scales[i / 2 % 2][i & 1]);
+                for (int i = 0; i < 4 * HALVES; ++i) {
+                    float& v = x[i / 4][i % 4];
+                    v = __fmul_rn(v, scales[i / 2 % 2][i & 1]);
+                    high[i & 1] = fmaxf(high[i & 1], v);
+                }
                 raise(high);
-                weigh();
+                if (coarse()) highest = -1.f;
+#pragma unroll
+                for (int i = 0; i < 4 * HALVES; ++i) w[i / 4][i % 4] = ex2f(x[i / 4][i % 4] - ref[i & 1]);
                 if (ATTEND && __any_sync(0xffffffffu, far >= kSpan)) {
                     float s = 0.f;                           // the greatest scale (of those that are numbers)
 #pragma unroll

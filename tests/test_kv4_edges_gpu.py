@@ -162,3 +162,51 @@ def test_rows_of_zeros_among_values(ctx):
     s = Step(ctx, 1, 1, 2, 4, 128, 300, 20, counts=np.full((1, 1), 300, np.int32), values=V)
     s.run(True)
     check_outputs(s)
+
+
+def one_sided(ctx, sign, key_exponent, query_exponent, G, d, M=150, n_old=20):
+    """A step whose logits are +-15 n 2^(key_exponent + query_exponent) / sqrt(d), n of 1 to 17 from row to row, of kept rows and entries
+    alike: every one exact in bf16 and in 4 bits.  Returns it and the rows and entries with the greatest."""
+    K = torch.zeros(1, 1, 2, M, d)
+    n = torch.randint(1, 18, (2, M + n_old + 1), generator=torch.Generator().manual_seed(G))
+    n[:, ::5] = 1 if sign < 0 else 17
+    k = sign * 15.0 * n * 2.0 ** key_exponent
+    K[0, 0, :, :, 3] = k[:, :M]
+    q = torch.zeros(1, 1, 2 * G, d)
+    q[..., 3] = 2.0 ** query_exponent
+    s = Step(ctx, 1, 1, 2, G, d, M, n_old, counts=np.full((1, 1), M, np.int32), keys=bf(K).cuda(), q=bf(q).cuda())
+    s.Kd.zero_(), s.k.zero_()
+    s.Kd[0, 0, :, :n_old, 3] = k[:, M:M + n_old].to(torch.bfloat16).cuda()
+    s.k[0, 0, :, 3] = k[:, -1].to(torch.bfloat16).cuda()
+    return s, (n == (1 if sign < 0 else 17)).numpy()
+
+
+def check_one_sided(s, wins, attend, off):
+    """Of a row's weights those of the greatest logits are alike, the others are 0; `off` is how far a weight may be from its own,
+    relative to it (2^-20 for the exponential and the division, and 32 bits' sums)."""
+    off += (wins.shape[1] + 8) * 2.0 ** -23 + 2.0 ** -19
+    n = s.n_old + 1
+    weight = wins / wins.sum(1, keepdims=True)                          # [Hkv, M + n]
+    old = np.append(s.before[0, 0, :n - 1], 0.0)
+    want = old + s.G * weight[:, s.M:].sum(0)
+    assert np.all(np.abs(s.acc.cpu().numpy()[0, 0, :n] - want) <= off * want)
+    if attend:
+        v = np.concatenate([R.values_of(f64(s.V[0, 0]), False), f64(s.Vd[0, 0, :, :n])], 1)
+        size = np.concatenate([R.sizes_of(f64(s.V[0, 0]), False), np.abs(f64(s.Vd[0, 0, :, :n]))], 1)
+        o, o_off = (np.einsum("ht,htd->hd", weight, t).repeat(s.G, 0) for t in (v, size))
+        assert np.all(np.abs(s.out.cpu().numpy()[0, 0] - o) <= off * o_off)
+
+
+@pytest.mark.parametrize("attend", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 7])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("exponents", [(0, 12), (11, 11), (14, 14), (17, 19), (20, 20), (30, 30), (50, 50), (60, 46), (-20, 119), (10, 100)])
+def test_logits_of_any_size(ctx, exponents, sign, G, d, attend):
+    """Those of 2^24 and more are apart by more than 32 bits' steps of one there, those of some -10^30 lie below what a row begins with."""
+    s, wins = one_sided(ctx, sign, *exponents, G, d)
+    s.run(attend)
+    # a logit, in units of powers of two, is rounded once on the way to an entry's weight, by 2^-24 of itself; from 2^23 on all are
+    # rounded alike
+    largest = 15 * (1 if sign < 0 else 17) * 2.0 ** sum(exponents) / np.sqrt(d) * 1.4427
+    check_one_sided(s, wins, attend, 2.0 ** -23 * largest if largest < 2.0 ** 23 else 0.0)
