@@ -213,7 +213,9 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const int power = min(max((int)(__float_as_uint(top) >> 23), 27), 254) - 141;          // top is about 2^(power + 14)
         const float down = __uint_as_float((uint32_t)(127 - power) << 23);                     // 2^-power
-        const float scale = p.scale_log2 * 0x1p24f * __uint_as_float((uint32_t)(127 + power) << 23);
+        // of a query row beyond 2^115, whose factor is beyond float32, its negative without 2^24
+        float scale = p.scale_log2 * __uint_as_float((uint32_t)(127 + power) << 23);
+        scale *= power > 100 ? -1.f : 0x1p24f;
 #pragma unroll
         for (int r = 0; r < 2; ++r) scale2[r] = __shfl_sync(0xffffffffu, scale, 8 * t4 + 4 * r);
 #pragma unroll
@@ -372,7 +374,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
         for (int r = 0; r < 2; ++r) large |= ref[r] != kUnset && fabsf(ref[r]) >= kCoarse;
         return (bool)__any_sync(0xffffffffu, large);
     };
-    float highest = coarse() ? -1.f : kHighest;              // what a tile's weights may be: below zero, each is looked at again
+    // what a tile's weights may be: below zero, each is looked at again
+    float highest = coarse() || __any_sync(0xffffffffu, fminf(scale2[0], scale2[1]) < 0.f) ? -1.f : kHighest;
     // in registers that the compiler cannot make anew for each use
     Under under = codes_under();
     under.k1024 |= (uint32_t)p.nsplit >> 31, under.k1032 |= (uint32_t)p.nsplit >> 31;
@@ -501,7 +504,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 #pragma unroll
                 for (int i = 0; i < 4 * HALVES; ++i) {
                     float& v = x[i / 4][i % 4];
-                    v = __fmul_rn(v, scales[i / 2 % 2][i & 1]);
+                    const float scale = scales[i / 2 % 2][i & 1];
+                    v = __fmul_rn(v, scale) * (scale < 0.f ? -0x1p24f : 1.f);
                     high[i & 1] = fmaxf(high[i & 1], v);
                 }
                 raise(high);

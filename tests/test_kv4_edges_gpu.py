@@ -210,3 +210,16 @@ def test_logits_of_any_size(ctx, exponents, sign, G, d, attend):
     # rounded alike
     largest = 15 * (1 if sign < 0 else 17) * 2.0 ** sum(exponents) / np.sqrt(d) * 1.4427
     check_one_sided(s, wins, attend, 2.0 ** -23 * largest if largest < 2.0 ** 23 else 0.0)
+
+
+@pytest.mark.parametrize("attend", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G", [4, 7])
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("exponents", [(-92, 114), (-92, 115), (-97, 120), (-100, 122), (-100, 127), (-60, 125), (-7, 121)])
+def test_queries_of_any_size(ctx, exponents, sign, G, d, attend):
+    """Queries up to bf16's largest, some heads' a little smaller.  (Keys in 4 bits are multiples of 2^-100, so all logits are beyond 2^23.)"""
+    s, wins = one_sided(ctx, sign, *exponents, G, d)
+    s.q[0, 0, 1::2] *= 2.0 ** -4
+    s.run(attend)
+    check_one_sided(s, wins, attend, 0.0)
