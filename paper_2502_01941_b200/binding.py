@@ -449,8 +449,8 @@ def shotkv_decode_step_attend(ctx: Context, state: DecodeState, q, k_new, v_new,
 
 # ------------------------------------------------------------------ norm, rotation, layout; the prompt in 4 bits
 def make_rope(rows=1, rot=0, first=0, layer=0, interleaved=False, eps=1e-6) -> Rope:
-    """What shotkv_norm_rope does; each call fills in the strides and the table's rows from the tensors it is given, so calls of
-    two threads take one each."""
+    """What shotkv_norm_rope does; the strides and the table's rows are those of the tensors that a call is given, and are not looked at
+    here."""
     return Rope(int(layer), int(first), int(rows), int(rot), int(bool(interleaved)), 0, float(eps))
 
 
@@ -474,6 +474,7 @@ def shotkv_norm_rope(ctx: Context, dims: Dims, rope: Rope, q, k, v, q_weight, k_
         rc = _native.norm_rope(ctx._h, dims, rope, q, k, v, q_weight, k_weight, cos_sin, positions, Qwin, K, V, q_out, stream)
         if rc is not None:
             return ctx.check(rc)
+    rope = Rope.from_buffer_copy(rope)                       # the caller's may be in another call, too
     qp, rope.q_row, rope.q_prompt = _heads(q, rope.rows, dims.H, dims.d, dims.B, "q")
     kp, rope.k_row, rope.k_prompt = _heads(k, rope.rows, dims.Hkv, dims.d, dims.B, "k")
     vp, rope.v_row, rope.v_prompt = _heads(v, rope.rows, dims.Hkv, dims.d, dims.B, "v")

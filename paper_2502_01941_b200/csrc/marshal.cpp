@@ -109,18 +109,18 @@ struct Args {
         return static_cast<const shotkv_bf16*>(t.data_ptr());
     }
     // [table rows][rot / 2][2], or None
-    const float* table(shotkv_rope* r) {
+    const float* table(shotkv_rope& r) {
         if (ok && i < n && a[i] == Py_None) {
             ++i;
-            r->table_rows = 0;
+            r.table_rows = 0;
             return nullptr;
         }
         const at::Tensor* t = cuda_tensor();
-        if (!ok || t->scalar_type() != at::kFloat || t->dim() != 3 || t->size(1) != r->rot / 2 || t->size(2) != 2 || t->size(0) > INT32_MAX) {
+        if (!ok || t->scalar_type() != at::kFloat || t->dim() != 3 || t->size(1) != r.rot / 2 || t->size(2) != 2 || t->size(0) > INT32_MAX) {
             ok = false;
             return nullptr;
         }
-        r->table_rows = (int32_t)t->size(0);
+        r.table_rows = (int32_t)t->size(0);
         return static_cast<const float*>(t->data_ptr());
     }
     void* raw(size_t& bytes) {
@@ -273,17 +273,19 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(a, n, [](Args& g) {
         auto* c = g.context();
         auto* d = g.structure<shotkv_dims>(g_dims);
-        auto* r = g.structure<shotkv_rope>(g_rope);
+        const auto* rope = g.structure<shotkv_rope>(g_rope);
+        shotkv_rope r{};                         // a copy: the caller's may be in another call, too
         const shotkv_bf16 *q = nullptr, *k = nullptr, *v = nullptr;
-        if (g.ok) q = g.heads(d, r->rows, d->H, r->q_row, r->q_prompt);
-        if (g.ok) k = g.heads(d, r->rows, d->Hkv, r->k_row, r->k_prompt);
-        if (g.ok) v = g.heads(d, r->rows, d->Hkv, r->v_row, r->v_prompt);
+        if (g.ok) r = *rope;
+        if (g.ok) q = g.heads(d, r.rows, d->H, r.q_row, r.q_prompt);
+        if (g.ok) k = g.heads(d, r.rows, d->Hkv, r.k_row, r.k_prompt);
+        if (g.ok) v = g.heads(d, r.rows, d->Hkv, r.v_row, r.v_prompt);
         auto *qw = g.bf16(), *kw = g.bf16();
         const float* cs = g.ok ? g.table(r) : nullptr;
         auto* pos = g.i32();
         auto *Q = g.bf16(), *K = g.bf16(), *V = g.bf16(), *qo = g.bf16();
         void* st = g.stream();
-        return [=] { return g_norm_rope(c, d, r, q, k, v, qw, kw, cs, pos, Q, K, V, qo, st); };
+        return [=] { return g_norm_rope(c, d, &r, q, k, v, qw, kw, cs, pos, Q, K, V, qo, st); };
     });
 }
 PyObject* compact_kv4(PyObject*, PyObject* const* a, Py_ssize_t n) {
