@@ -469,7 +469,8 @@ def _heads(t, rows, heads, d, B, name):
 
 def shotkv_norm_rope(ctx: Context, dims: Dims, rope: Rope, q, k, v, q_weight, k_weight, cos_sin, positions, Qwin, K, V, q_out=None,
                      stream=None) -> int:
-    """q [B, rows, H, d], k and v [B, rows, Hkv, d] may be views of one projection; cos_sin [table rows, rot / 2, 2]."""
+    """q [B, rows, H, d], k and v [B, rows, Hkv, d] may be views of one projection; cos_sin [table rows, rot / 2, 2]; positions
+    [B, rows]."""
     if _native is not None:
         rc = _native.norm_rope(ctx._h, dims, rope, q, k, v, q_weight, k_weight, cos_sin, positions, Qwin, K, V, q_out, stream)
         if rc is not None:
@@ -481,8 +482,11 @@ def shotkv_norm_rope(ctx: Context, dims: Dims, rope: Rope, q, k, v, q_weight, k_
     if cos_sin is not None and tuple(cos_sin.shape[1:]) != (rope.rot // 2, 2):
         raise ValueError(f"cos_sin: expected shape [rows, {rope.rot // 2}, 2], got {tuple(cos_sin.shape)}")
     rope.table_rows = 0 if cos_sin is None else cos_sin.shape[0]
+    at = _dev(positions, _I32, "positions")
+    if positions is not None and positions.numel() != dims.B * rope.rows:
+        raise ValueError(f"positions: expected shape {(dims.B, rope.rows)}, got {tuple(positions.shape)}")
     rc = lib().shotkv_norm_rope(ctx._h, C.byref(dims), C.byref(rope), qp, kp, vp, _dev(q_weight, _BF16, "q_weight"),
-                                _dev(k_weight, _BF16, "k_weight"), _dev(cos_sin, _F32, "cos_sin"), _dev(positions, _I32, "positions"),
+                                _dev(k_weight, _BF16, "k_weight"), _dev(cos_sin, _F32, "cos_sin"), at,
                                 _dev(Qwin, _BF16, "Qwin"), _dev(K, _BF16, "K"), _dev(V, _BF16, "V"), _dev(q_out, _BF16, "q_out"),
                                 _stream(stream))
     return ctx.check(rc)

@@ -123,6 +123,17 @@ struct Args {
         r.table_rows = (int32_t)t->size(0);
         return static_cast<const float*>(t->data_ptr());
     }
+    // [B][rows], or None
+    const int32_t* positions(const shotkv_dims* dims, int rows) {
+        if (ok && i < n && a[i] != Py_None) {
+            if (!THPVariable_CheckExact(a[i])) {
+                ok = false;
+                return nullptr;
+            }
+            ok = THPVariable_Unpack(a[i]).numel() == (int64_t)dims->B * rows;
+        }
+        return i32();
+    }
     void* raw(size_t& bytes) {
         const at::Tensor* t = cuda_tensor();
         if (!ok) return nullptr;
@@ -282,7 +293,7 @@ PyObject* norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (g.ok) v = g.heads(d, r.rows, d->Hkv, r.v_row, r.v_prompt);
         auto *qw = g.bf16(), *kw = g.bf16();
         const float* cs = g.ok ? g.table(r) : nullptr;
-        auto* pos = g.i32();
+        const int32_t* pos = g.ok ? g.positions(d, r.rows) : nullptr;
         auto *Q = g.bf16(), *K = g.bf16(), *V = g.bf16(), *qo = g.bf16();
         void* st = g.stream();
         return [=] { return g_norm_rope(c, d, &r, q, k, v, qw, kw, cs, pos, Q, K, V, qo, st); };

@@ -71,3 +71,23 @@ def test_threads_share_a_description(way):
     for t in threads:
         t.join()
     assert not errors, errors[0]
+
+
+def test_positions_are_those_of_every_prompt_and_row(ctx, way):
+    """One row of positions for all prompts is not expanded: it is refused, as is any other number of them."""
+    s = Layer(2, 1, 8, 2, 64, 50, 9, 2, 40, 64, given=True)
+    good = s.positions
+    for bad in (good[:1], good[0], good[:, :39].contiguous(), torch.cat([good, good[:1]]), good[:0]):
+        s.positions = bad
+        with pytest.raises(ValueError, match="positions"):
+            s.run(ctx)
+    for bad in ([0] * 80, good.long(), good.float()):
+        s.positions = bad
+        with pytest.raises(TypeError, match="positions"):
+            s.run(ctx)
+    for same in (good, good.flatten()):
+        s.positions = same
+        s.K.fill_(7), s.V.fill_(7), s.Qwin.fill_(7)
+        s.run(ctx)
+        s.positions = good
+        s.check()
