@@ -250,7 +250,13 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     // of query rows 2*t4 and 2*t4 + 1: the reference (the same in the 8 lanes of a t4), this lane's part of the sum of p, and of w z_v
     float ref[2] = {kUnset, kUnset}, z[2] = {0.f, 0.f}, wz[2] = {0.f, 0.f};
     constexpr int kFirstLane = PAIRED ? 2 : 4;               // lanes a row's keys are spread over: those of one t4, or of t4 and t4 ^ 2
+    // What a tile's weights may be.  From 2^22 on a logit's own rounding counts: as a multiply-add its weight would be that of the exact
+    // product, apart from the reference by up to half a step of 32 bits.  So a warp that has met one so large, or a query row whose
+    // factor is in two parts, looks at every tile again, where logits are rounded before the reference is subtracted, as the
+    // entries' are.
+    float highest = __any_sync(0xffffffffu, fminf(scale2[0], scale2[1]) < 0.f) ? -1.f : kHighest;
     const auto raise = [&](const float (&high)[2]) {         // new references, from all lanes' greatest logits
+        bool coarse = false;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             float m = high[r];
@@ -260,12 +266,14 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
             const float up = fmaxf(ref[r], fabsf(m) < 0x1p27f ? m - kLift : m);
             const float al = ex2f(ref[r] - up);
             ref[r] = up;
+            coarse |= up != kUnset && fabsf(up) >= kCoarse;
             z[r] *= al;
             wz[r] *= al;
             if (ATTEND)
 #pragma unroll
                 for (int mt = 0; mt < MT; ++mt) O[mt][r] *= al, O[mt][2 + r] *= al;
         }
+        if (__any_sync(0xffffffffu, coarse)) highest = -1.f;
     };
 
     // ---- decode entries
@@ -365,17 +373,6 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
     if (ATTEND)                                              // odd dimensions' are sixteen times as much from here on
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) O[mt][2] *= 16.f, O[mt][3] *= 16.f;
-    // From 2^22 on a logit's own rounding counts: as a multiply-add its weight would be that of the exact product, apart from the
-    // reference by up to half a step of 32 bits.  So a warp that has met one so large looks at every tile again, where logits
-    // are rounded before the reference is subtracted, as the entries' are.
-    const auto coarse = [&] {
-        bool large = false;
-#pragma unroll
-        for (int r = 0; r < 2; ++r) large |= ref[r] != kUnset && fabsf(ref[r]) >= kCoarse;
-        return (bool)__any_sync(0xffffffffu, large);
-    };
-    // what a tile's weights may be: below zero, each is looked at again
-    float highest = coarse() || __any_sync(0xffffffffu, fminf(scale2[0], scale2[1]) < 0.f) ? -1.f : kHighest;
     // in registers that the compiler cannot make anew for each use
     Under under = codes_under();
     under.k1024 |= (uint32_t)p.nsplit >> 31, under.k1032 |= (uint32_t)p.nsplit >> 31;
@@ -509,7 +506,6 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     high[i & 1] = fmaxf(high[i & 1], v);
                 }
                 raise(high);
-                if (coarse()) highest = -1.f;
 #pragma unroll
                 for (int i = 0; i < 4 * HALVES; ++i) w[i / 4][i % 4] = ex2f(x[i / 4][i % 4] - ref[i & 1]);
                 if (ATTEND && __any_sync(0xffffffffu, far >= kSpan)) {
@@ -525,17 +521,22 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                     for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
                     const uint32_t e = min(max(__float_as_uint(s) >> 23, 27u), 250u);      // its exponent
                     unit = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
-                    // a row whose scale is small beside it is added by itself
+                    // rows whose scale is small beside it are added by themselves
+                    const auto small = [&](uint32_t word) { return word != 0 && (int)above(word) < 0; };
+                    bool some = false;
 #pragma unroll
-                    for (int h = 0; h < HALVES; ++h)
+                    for (int i = 0; i < 2 * HALVES; ++i) some |= small(vw[i / 2][i % 2]);
+                    if (__any_sync(0xffffffffu, some))
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const bool alone = vw[h][k] != 0 && (int)above(vw[h][k]) < 0;
-                            uint32_t lanes = __ballot_sync(0xffffffffu, alone) & (PAIRED ? 0x55555555u : 0x11111111u);
+                        for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const bool alone = small(vw[h][k]);
+                                uint32_t lanes = __ballot_sync(0xffffffffu, alone) & (PAIRED ? 0x55555555u : 0x11111111u);
 #pragma unroll 1
-                            for (; lanes; lanes &= lanes - 1) add_row(st, __ffs(lanes) - 1, h, k, w[h][2 * k], w[h][2 * k + 1], vw[h][k]);
-                            if (alone) vw[h][k] = 0;
-                        }
+                                for (; lanes; lanes &= lanes - 1) add_row(st, __ffs(lanes) - 1, h, k, w[h][2 * k], w[h][2 * k + 1], vw[h][k]);
+                                if (alone) vw[h][k] = 0;
+                            }
                 }
             }
         }
