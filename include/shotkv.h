@@ -123,7 +123,8 @@ typedef struct {
 
 /* Queries and keys normed per head and rotated by position, values as they are, each written where the other calls
  * read it: what stands between a layer's projection and the prefill calls, or (with N = W = rows = 1) the decode
- * step.  Per head of d elements, in 32 bits, rounded to bf16 once:
+ * step.  Per head of d elements, in 32 bits (the squares, too: nothing beyond 2^60 in a head that is normed), rounded to
+ * bf16 once:
  *   y = x / sqrt(mean(x^2) + eps) * weight          where a weight is given, else y = x
  *   (a, b) -> (a cos - b sin, b cos + a sin)        for the pairs of the first rot elements
  *   q, k, v    device bf16, heads of d contiguous elements: head h of row r of prompt b at
@@ -317,7 +318,8 @@ SHOTKV_API int shotkv_decode_step_attend(shotkv_ctx* ctx, shotkv_decode_state* s
  *   s      the least bf16 number that is no less than (max - min) / 15, max|x| / 240 and 2^-100 of the group,
  *   c + z  = floor(x / s + 1/2),   z = 8 + the group's least such number.
  * So an element is off by at most s / 2, every row stands by itself, and what is read is what is meant: s * (c + z) is
- * exact in 32 bits.  A group with an element that is not finite, or whose range is beyond float32, reads as NaN.
+ * exact in 32 bits (an element beyond 1.85 * 2^127 may read as infinite).  A group with an element that is not finite, or
+ * whose range is beyond float32, reads as NaN.
  * Keys and values of a unit (b, l, g) are ceil(Mcap / 32) tiles of 32 rows each, base addresses 16-byte aligned:
  *   K4  device [B][L][Hkv][tiles][32 * (d/2 + d/8)] bytes      V4  device [B][L][Hkv][tiles][32 * (d/2 + 4)] bytes
  * A tile is its codes as 32-bit words, then one word per group, row by row: s in the high half, z in the low half, both
@@ -353,7 +355,12 @@ SHOTKV_API int shotkv_prefill_compress_kv4(shotkv_ctx* ctx, const shotkv_dims* d
 /* shotkv_decode_step and shotkv_decode_step_attend with the compressed prompt in 4 bits (state->Mcap its rows, kept_count
  * as there); the decode entries are bf16 as there, and state, eviction and outputs are the same.  A step may change from
  * one form of the prompt to the other between calls.  Logits and outputs are sums in 32 bits over s * (c + z) as it
- * stands: nothing is rounded on the way but the weights of the output, to 22 bits.  */
+ * stands, of which matrix units cut off what does not fit; what is rounded on the way is
+ *   queries   elements below 2^-31 of their row's largest, to 2^-39 of it;
+ *   weights   of the output, to 2^-22 of themselves or, where that is more, 2^-35 of their row's largest, and 2^-27 of it
+ *             where values' scales differ by 2^8 and more (2^-25 and 2^-17 where log2(e) times the largest logit is 2^27 or more).
+ * s * c and s * z are added apart, so where |z| is large an error is one of s * (|c| + |z|).  Values beyond 2^80 in magnitude may
+ * leave float32's range on the way.  */
 SHOTKV_API int shotkv_decode_step_kv4(shotkv_ctx* ctx, shotkv_decode_state* state,
                            const shotkv_bf16* q, const shotkv_bf16* k_new, const shotkv_bf16* v_new,
                            const void* K4, const int32_t* kept_count, void* stream);
@@ -393,7 +400,7 @@ SHOTKV_API uint64_t shotkv_repaired_items(const shotkv_ctx* ctx);
 /* Failure detection.  The tensor-core kernels of this library (the scoring pass of Section 5.1's
  * prefill score equation and the per-token second pass) hand tiles between warps through shared-
  * memory barriers; the CTAs of a cluster in the reduction and the decode steps wait for one another's
- * messages.  Every such wait is bounded: after `cycles` SM clock cycles (default 4e9, about
+ * messages, and the warps of the steps over a packed prompt for their tiles.  Every such wait is bounded: after `cycles` SM clock cycles (default 4e9, about
  * two seconds) the waiting warp gives up, raises its CTA's abort flag and a host-visible error
  * word, all roles leave their loops, copies and messages in flight are waited for (about two seconds at most, whatever
  * the limit: they write into the CTA's memory), tensor memory is released and the kernel returns.  The next call on the context then returns

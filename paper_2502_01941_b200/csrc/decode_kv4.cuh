@@ -95,7 +95,7 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 // PAIRED, for groups of up to four rows: the columns 4 .. 7 are the same rows again.  The remainders are in these columns of the one
 // operand whose columns 0 .. 3 are the high parts, so that one product does for both, and the lanes of columns 0 .. 3 have the
 // logits of one half of a tile, those of columns 4 .. 7 of the other.  (8 sequences x 32 layers, 3,276 rows, 145
-// entries, four query rows: 189 us a step, 217 without.)
+// entries, captured: four query rows 186 us a step, eight, each half and part with products of its own, 219.)
 //
 // f16 ends at 65504, so both factors are kept in range by references that change seldom: a row's reference is 2^10 below its
 // maximum when it was last set and is set again by a tile whose p would exceed 2^13, and the values' scales are multiplied by a
@@ -104,10 +104,11 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 // largest (2^-35 where the scales are alike), whatever the others' values are.  One vote a tile
 // decides that nothing of this has happened.  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
 // products are summed for themselves and then added: one sum for all of a warp's 26 tiles left the outputs 4.2e-6 off in the
-// 2-norm, so they are 5.5e-7 off (elementary operations in 32 bits: 9.3e-7).
+// 2-norm, so they are 5.5e-7 off (elementary operations in 32 bits: 9.2e-7).  Scores are 2.6e-7 off (1.5e-7): s (c + 8) . q and s (z - 8)
+// times the sum of q are rounded apart.
 //
 // What bounds it: bytes from HBM where calls are far apart (that step reads 1.09 GB: 178 us with kept counts that differ, 6.1 TB/s), and
-// the power cap where they follow one another for long (199 to 210 us from GPU to GPU, at 1.6 to 1.7 GHz): about 480 instructions a tile, half of them
+// the power cap where they follow one another for long (198 to 210 us from GPU to GPU, at 1.6 to 1.7 GHz): about 480 instructions a tile, half of them
 // conversions and the groups' scales, at 0.6 to 0.7 a cycle and scheduler.  So what was saved is instructions (780 at first): bulk
 // copies that one lane asks for, no accumulator set to zero, constants that stay in registers, sums of two rows at a time.  More
 // CTAs on an SM, or one tile's values computed beside the next one's keys, gained nothing.  Scores alone read half: 96 us, 6.0 TB/s.

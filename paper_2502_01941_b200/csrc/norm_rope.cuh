@@ -32,7 +32,8 @@ struct NormRopeParams {
 // rot / 16 away, of neighbours from the same word.
 // 4 x 32,768 rows of 8 KV heads 178 us, 6.1 TB/s read and written (keys and values in warps of their own, one row at a time: 230;
 // CTAs of 256 threads: 182); 4,096 rows with all of 32 heads' queries 22 us, 4.7 TB/s: three and a half waves of warps; eight
-// single rows 2.4 us.
+// single rows 2.4 us.  The bound of six CTAs an SM leaves 80 registers, and 508 bytes a thread are spilled and 768 read back (d = 64
+// and 128 alike).  Of five, 96 registers and nothing spilled, it measures 173, 20.7 and 2.35 us.
 constexpr int kRopeThreads = 128, kRopeAhead = 4;
 template <int D>
 __host__ __device__ constexpr int rope_heads_a_piece() { return 32 / (D / 8); }
