@@ -99,10 +99,11 @@ __host__ __device__ constexpr size_t kv4_smem_bytes(int G, int Dcap, int nsplit)
 //
 // f16 ends at 65504, so both factors are kept in range by references that change seldom: a row's reference is 2^10 below its
 // maximum when it was last set and is set again by a tile whose p would exceed 2^13, and the values' scales are multiplied by a
-// power of two that takes the largest of the first tile to [1, 2) and is set again by a tile with a scale outside [2^-8, 4); if the tile's
-// own scales are that far apart, its rows of small scale are added by themselves.  So a weight is off by no more than 2^-27 of the row's
-// largest (2^-35 where the scales are alike), whatever the others' values are.  One vote a tile
-// decides that nothing of this has happened.  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
+// power of two that takes the largest of the first tile to [1, 2) and is set again by a tile more than half of whose scales it leaves
+// outside [2^-8, 4); a tile's rows that are outside are added by themselves.  So a weight is off by no
+// more than 2^-27 of the row's largest (2^-35 where the scales are alike), whatever the others' values are.  One vote a tile
+// decides that nothing of this has happened.  (8 sequences x 32 layers, 3,276 rows, one value in 1,000, in 32, in 8 of 2^10 or 2^-10
+// of the others' scale: 189, 250, 377 us.)  A matrix unit cuts off what does not fit its sums, always towards zero, so a tile's
 // products are summed for themselves and then added: one sum for all of a warp's 26 tiles left the outputs 4.2e-6 off in the
 // 2-norm, so they are 5.5e-7 off (elementary operations in 32 bits: 9.2e-7).  Scores are 2.6e-7 off (1.5e-7): s (c + 8) . q and s (z - 8)
 // times the sum of q are rounded apart.
@@ -510,30 +511,42 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
 #pragma unroll
                 for (int i = 0; i < 4 * HALVES; ++i) w[i / 4][i % 4] = ex2f(x[i / 4][i % 4] - ref[i & 1]);
                 if (ATTEND && __any_sync(0xffffffffu, far >= kSpan)) {
-                    float s = 0.f;                           // the greatest scale (of those that are numbers)
+                    // Other units where these do for less than half of the tile's rows: those of the greatest scale, or if they
+                    // do not do either of the greatest below them, and so on.  Rows that the units do not do for are added by themselves.
+                    constexpr uint32_t kOnce = PAIRED ? 0x55555555u : 0x11111111u;        // of the lanes with a row's word one
 #pragma unroll
-                    for (int h = 0; h < HALVES; ++h)
+                    for (int i = 0; i < 2 * HALVES; ++i)
+                        if (tile * 32 + half_of(i / 2) * 16 + g + 8 * (i % 2) >= M) vw[i / 2][i % 2] = 0;
+                    uint32_t below = 0x7f800000u;            // (so of the scales that are numbers)
+#pragma unroll 1
+                    for (;;) {
+                        int fit = 0;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            if (tile * 32 + half_of(h) * 16 + g + 8 * k >= M) vw[h][k] = 0;
-                            s = fmaxf(s, bf16_high(vw[h][k]));
-                        }
+                        for (int i = 0; i < 2 * HALVES; ++i)
+                            fit += __popc(__ballot_sync(0xffffffffu, above(vw[i / 2][i % 2]) < kSpan) & kOnce);
+                        if (2 * fit >= min(32, M - tile * 32)) break;
+                        float s = 0.f;
 #pragma unroll
-                    for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
-                    const uint32_t e = min(max(__float_as_uint(s) >> 23, 27u), 250u);      // its exponent
-                    unit = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
-                    // rows whose scale is small beside it are added by themselves
-                    const auto small = [&](uint32_t word) { return word != 0 && (int)above(word) < 0; };
+                        for (int i = 0; i < 2 * HALVES; ++i)
+                            s = fmaxf(s, vw[i / 2][i % 2] < below ? bf16_high(vw[i / 2][i % 2]) : 0.f);
+#pragma unroll
+                        for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
+                        if (s == 0.f) break;
+                        const uint32_t e = min(max(__float_as_uint(s) >> 23, 27u), 250u);  // its exponent
+                        unit = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
+                        below = (e - 8) << 23;
+                    }
+                    const auto apart = [&](uint32_t word) { return word != 0 && above(word) >= kSpan; };
                     bool some = false;
 #pragma unroll
-                    for (int i = 0; i < 2 * HALVES; ++i) some |= small(vw[i / 2][i % 2]);
+                    for (int i = 0; i < 2 * HALVES; ++i) some |= apart(vw[i / 2][i % 2]);
                     if (__any_sync(0xffffffffu, some))
 #pragma unroll
                         for (int h = 0; h < HALVES; ++h)
 #pragma unroll
                             for (int k = 0; k < 2; ++k) {
-                                const bool alone = small(vw[h][k]);
-                                uint32_t lanes = __ballot_sync(0xffffffffu, alone) & (PAIRED ? 0x55555555u : 0x11111111u);
+                                const bool alone = apart(vw[h][k]);
+                                uint32_t lanes = __ballot_sync(0xffffffffu, alone) & kOnce;
 #pragma unroll 1
                                 for (; lanes; lanes &= lanes - 1) add_row(st, __ffs(lanes) - 1, h, k, w[h][2 * k], w[h][2 * k + 1], vw[h][k]);
                                 if (alone) vw[h][k] = 0;
