@@ -531,8 +531,8 @@ decode_kv4_kernel(const DecodeParams p, const DecodeFinishParams f, const Packed
                             s = fmaxf(s, vw[i / 2][i % 2] < below ? bf16_high(vw[i / 2][i % 2]) : 0.f);
 #pragma unroll
                         for (int o = kFirstLane; o <= 16; o <<= 1) s = fmaxf(s, __shfl_xor_sync(0xffffffffu, s, o));
-                        if (s == 0.f) break;
-                        const uint32_t e = min(max(__float_as_uint(s) >> 23, 27u), 250u);  // its exponent
+                        if (!(s >= 0x1p-100f)) break;        // none, or what was never packed: every turn goes lower, to here
+                        const uint32_t e = min(__float_as_uint(s) >> 23, 250u);            // its exponent, 27 or more
                         unit = __uint_as_float((254 - e) << 23), back = __uint_as_float(e << 23);
                         below = (e - 8) << 23;
                     }

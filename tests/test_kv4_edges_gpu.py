@@ -223,3 +223,34 @@ def test_queries_of_any_size(ctx, exponents, sign, G, d, attend):
     s.q[0, 0, 1::2] *= 2.0 ** -4
     s.run(attend)
     check_one_sided(s, wins, attend, 0.0)
+
+
+@pytest.mark.parametrize("attend", [False, True])
+@pytest.mark.parametrize("G", [4, 7])
+@pytest.mark.parametrize("words", ["bytes", "zeros", "least", "below", "greatest", "negative", "nan", "mixed"])
+def test_a_cache_that_was_never_packed_ends_the_step(ctx, words, G, attend):
+    """What such a step gives is of no meaning, but it ends, and it leaves the entries' rows, other units and the next step as they are."""
+    M, n_old = 300, 20
+    s = Step(ctx, 1, 1, 2, G, 64, M, n_old, counts=np.full((1, 1), M, np.int32))
+    good = s.K4.clone(), s.V4.clone()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    tile = s.V4[0, 0, 0].view(torch.int32)[:, 4 * 64:]                    # one unit's words of the values' scales
+    fill = {"zeros": 0, "least": 1, "below": (20 << 23) | 5, "greatest": 0x7F7FFFFF, "negative": -(1 << 31) + (100 << 23), "nan": 0x7FC00001}
+    if words == "bytes":
+        for t in (s.K4, s.V4):
+            t[0, 0, 0] = torch.randint(0, 256, t[0, 0, 0].shape, generator=g, device="cuda", dtype=torch.uint8)
+    elif words == "mixed":
+        tile.copy_(torch.tensor(list(fill.values()), device="cuda", dtype=torch.int32).repeat(tile.numel() // 6 + 1)[:tile.numel()].view_as(tile))
+    else:
+        tile.fill_(fill[words])
+    s.run(attend)
+    torch.cuda.synchronize()
+    assert torch.equal(s.Kd[:, :, :, n_old], s.k) and torch.equal(s.Vd[:, :, :, n_old], s.v)
+    bad = s.out.clone()
+    s.K4.copy_(good[0]), s.V4.copy_(good[1])
+    s.st.T = s.st.n_dec = n_old
+    s.acc.copy_(torch.from_numpy(s.before))
+    s.run(attend)
+    s.check(attend)
+    if attend:
+        assert torch.equal(bad[0, 0, G:], s.out[0, 0, G:])                # the other unit's
